@@ -18,7 +18,10 @@
  *   dssd_dsd_verify       the fused verification of Algorithm 1 (no row is transmitted);
  *   dssd_edge_partial, dssd_edge_combine, dssd_edge_emit_shard, dssd_resample_shard_mass,
  *   dssd_resample_shard_draw
- *                         the round for an edge whose vocabulary is sharded over several GPUs.
+ *                         the round for an edge whose vocabulary is sharded over several GPUs;
+ *   dssd_adjust_logits, dssd_tree_attention, dssd_tree_verify, dssd_cache_append
+ *                         a round on a drafted tree: the target model's attention for its nodes, the logits
+ *                         made ready, the verdict, and the accepted path's keys and values into the cache.
  *
  * Notation follows the paper: gamma draft tokens x_1..x_gamma with draft probabilities
  * q_i(x_i), target distributions P_1..P_{gamma+1} over a vocabulary of V entries, uniforms
@@ -66,7 +69,8 @@ typedef enum {
 
 typedef enum {
     DSSD_F32 = 0, /* IEEE binary32 logits  */
-    DSSD_BF16 = 1 /* bfloat16 logits       */
+    DSSD_BF16 = 1, /* bfloat16 logits       */
+    DSSD_F16 = 2   /* IEEE binary16: dssd_tree_attention and dssd_cache_append only */
 } dssd_dtype;
 
 #define DSSD_MAX_V (1 << 30)
@@ -576,6 +580,167 @@ dssd_status dssd_resample_shard_draw(const double *masses, int G, int g, int v_b
                                      int gamma, int V_shard, int32_t *token, uint32_t *flags,
                                      const void *workspace, size_t workspace_bytes,
                                      void *cuda_stream);
+
+/*
+ * ---------------------------------------------------------------------------------------------
+ * A round on a drafted tree.
+ *
+ * The device may draft several candidates for a position.  They form a tree of N nodes per
+ * sequence: node 0, the root, is the last committed token; node j = 1 .. N-1 holds drafted token
+ * x_j and hangs under node parents[b, j-1], which has to be present and of a lower index.  A negative parent marks a
+ * place without a node (the batch may be ragged); parents == NULL is the chain 0 - 1 - ... - N-1 (gamma =
+ * N - 1).  A parent that is not below its node, or not present, takes the node out as a negative one does, and is
+ * reported in the flags.  Arrays of one value per drafted token, draft_tokens, parents and uniforms, are
+ * [B, N-1] (NULL iff N == 1): entry j-1 belongs to node j.
+ *
+ * The order of a round: per layer dssd_tree_attention (the nodes see the cache and their own ancestors), then
+ * dssd_adjust_logits on the N rows of logits, dssd_tree_verify, and dssd_cache_append for the keys
+ * and values of the accepted path.  A chain may use the calls above in dssd_tree_verify's place.
+ * ---------------------------------------------------------------------------------------------
+ */
+#define DSSD_TREE_MAX_NODES 128
+
+/* flags written by dssd_adjust_logits, one word per sequence */
+#define DSSD_ADJUST_FLAG_BAD_TOKEN 1u  /* a token of the history, the draft or the biases is outside [0, V): it counts for nothing */
+#define DSSD_ADJUST_FLAG_BAD_PARENT 2u /* see above */
+#define DSSD_ADJUST_FLAG_BAD_LENGTH 4u /* history_len outside [0, history width]: taken as the nearer end */
+#define DSSD_ADJUST_FLAG_BAD_VALUE 8u  /* a repetition penalty that is not a positive finite number: taken as 1 */
+#define DSSD_ADJUST_FLAG_BAD_MASK 16u  /* mask_row beyond the last mask: the row is not masked */
+
+/*
+ * Penalties for repeated tokens, biases and masks on the N rows of target logits of each sequence (chain: the
+ * gamma+1 positions), each row with the tokens drafted on its own way from the root counted as if they had
+ * been emitted.  For row j of sequence b and token v, with
+ *   n_out = occurrences of v in history[b, prompt_len .. history_len) and among the drafted
+ *           tokens of node j and its ancestors (the root's token is the history's last one),
+ *   n_all = n_out + occurrences in history[b, 0 .. prompt_len):
+ *   x = l;   if n_all > 0: x = x > 0 ? x / repetition : x * repetition;
+ *   x = x - frequency * n_out - (n_out > 0 ? presence : 0);   x = x + bias(v);
+ *   x = -inf if the row's mask does not allow v, whatever l holds.
+ * Computed in float32, rounded once to the type of the logits; a token that none of these concerns keeps its bits.
+ *
+ * logits        [B, N, V] float32 or bfloat16, row (b, j) at element (b*N+j)*row_stride
+ * draft_tokens, parents   see above
+ * history       [B, L] int32, history_stride elements between rows (NULL iff L == 0)
+ * prompt_len, history_len [B] int32 (NULL iff L == 0); a prompt_len beyond history_len is taken as history_len
+ * repetition, presence, frequency  [B] float32, each optional (NULL: 1, 0, 0)
+ * bias_tokens   [B, K] int32, bias_values [B, K] float32 (NULL iff K == 0; K <= 65535); negative
+ *               tokens are empty places; where a token appears twice, its last entry holds
+ * mask          [mask_rows, (V+31)/32] words, optional: bit v % 32 of word v / 32 is set where token v is allowed
+ * mask_row      [B, N] int32, the mask of each row, negative: none (NULL: row b*N+j; mask_rows >= B*N then)
+ * out           [B, N, V] of the same type, out_stride elements between rows.  out == logits (with the same
+ *               stride) works in place and touches only the entries that change.  Rows without a node are left
+ *               as they were.  Otherwise the two must not overlap.
+ * flags         [B] uint32 out, optional (NULL ok)
+ */
+dssd_status dssd_adjust_logits(const void *logits, dssd_dtype dtype, int64_t row_stride, int B, int N, int V,
+                               const int32_t *draft_tokens, const int32_t *parents,
+                               const int32_t *history, int64_t history_stride, int L, const int32_t *prompt_len,
+                               const int32_t *history_len, const float *repetition, const float *presence,
+                               const float *frequency, const int32_t *bias_tokens, const float *bias_values, int K,
+                               const uint32_t *mask, int mask_rows, const int32_t *mask_row, void *out,
+                               int64_t out_stride, uint32_t *flags, void *cuda_stream);
+
+/* flags of dssd_tree_attention and dssd_cache_append, one word per sequence */
+#define DSSD_CACHE_FLAG_BAD_PAGE 1u   /* a page number outside [0, num_pages): attention reads zeros there, append skips the row */
+#define DSSD_CACHE_FLAG_BAD_LENGTH 2u /* ctx_len negative or beyond the table's pages: taken as the nearer end; append skips
+                                         rows beyond the table */
+#define DSSD_CACHE_FLAG_BAD_NODE 4u   /* a parent that is no node below (attention); a path entry outside [0, N) (append) */
+
+/* Bytes of scratch that dssd_tree_attention needs (0 if the sizes are invalid).  Depends on the sizes only. */
+size_t dssd_tree_attention_workspace_bytes(int B, int N, int Hq, int Hkv, int D);
+
+/*
+ * Attention of the tree's nodes over a paged cache: node j sees the ctx_len[b] cached positions, its
+ * ancestors and itself.
+ *   o[b,j,h] = sum_t softmax_t(scale * q[b,j,h] . k_t) v_t,   key head h / (Hq/Hkv)
+ * Products of 16-bit values are accumulated in float32; the running maximum and sum are float32; the weights are
+ * rounded to the inputs' type before they meet v; o is rounded once more.
+ *
+ * q             [B, N, Hq, D], k_new, v_new [B, N, Hkv, D], o [B, N, Hq, D]: bfloat16 or binary16, unit stride along D; q_strides, new_strides,
+ *               o_strides (host): elements between sequences, nodes and heads
+ * k_cache, v_cache   [num_pages, page_size, Hkv, D] of the same type; cache_strides (host): elements between pages, positions and heads
+ * block_table   [B, max_pages] int32, table_stride elements between rows: position t of sequence b is in page
+ *               block_table[b, t / page_size].  Entries beyond ctx_len are not used
+ * ctx_len       [B] int32
+ * parents       [B, N-1] int32 or NULL (a chain)
+ * lse           [B, N, Hq] float32 out, optional (NULL ok): ln sum_t exp(scale * q . k_t)
+ * flags         [B] uint32 in/out, optional: bits are added to what it holds, so that the layers of a model share it
+ * Rows of o and lse without a node are left as they were.  What a sequence holds in unused
+ * positions of its pages has no effect, NaN included.  A node sees no value of a node that is not its ancestor, unless
+ * that value is infinite or NaN: then the rows of the whole sequence may be NaN.
+ * D is a multiple of 8, at most 128; Hq a multiple of Hkv with Hq/Hkv <= 128; 1 <= N <= DSSD_TREE_MAX_NODES.  Every pointer to q, k, v and o
+ * is 16-byte aligned and every stride a multiple of 8 elements (DSSD_ERR_UNSUPPORTED otherwise).
+ */
+dssd_status dssd_tree_attention(const void *q, const int64_t *q_strides, const void *k_new, const void *v_new,
+                                const int64_t *new_strides, const void *k_cache, const void *v_cache,
+                                const int64_t *cache_strides, dssd_dtype dtype, const int32_t *block_table,
+                                int64_t table_stride, int max_pages, int num_pages, int page_size,
+                                const int32_t *ctx_len, const int32_t *parents, int B, int N, int Hq, int Hkv,
+                                int D, float scale, void *o, const int64_t *o_strides, float *lse, uint32_t *flags,
+                                void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+#define DSSD_EDGE_FLAG_BAD_PARENT 8u /* dssd_tree_verify: see above */
+
+/* Bytes of scratch that dssd_tree_verify needs (0 if the sizes are invalid). */
+size_t dssd_tree_verify_workspace_bytes(int B, int N, int V);
+
+/*
+ * The verdict on a drafted tree and the token drawn after it: Algorithm 1's fused verification where a position
+ * has several candidates.  From the root on, the children of a node are tested in index order.
+ * With p the node's target distribution softmax(l / T), q the distribution that its children were drawn from, and
+ * a = 0, m = 1, c = 1 before its first child, child j is accepted iff
+ *   u_j * c * m * q(x_j) < max(0, p(x_j) - a * q(x_j)).
+ * After a rejection the residual distribution is max(0, p - a q) / m with
+ *   a <- a + c * m,  m <- sum_v max(0, p_v - a q_v),
+ * and, where siblings are drawn without replacement (replacement == 0), c <- 1 / (1 - sum of the q of the rejected siblings):
+ * p_{r+1} = norm(max(0, p_r - q_r)) for every r, in closed form.  An accepted child becomes the node; where no
+ * child is accepted (or there is none) the token is drawn from max(0, p - a q) with u', by inverse CDF
+ * in index order as dssd_device_resample does (the fallback to p included).  Every emitted token follows the target distribution.
+ * For a chain this is dssd_dsd_verify.
+ *
+ * Only the rows of nodes on the accepted path are read, and draft rows of those with a rejection.
+ * p, sums and the draw are evaluated in float64 (exponentials to about 1e-13).  u == 1 never accepts; q <= 0 accepts iff the left over p > 0; a
+ * NaN q or an out-of-range token rejects.
+ *
+ * target_logits [B, N, V] float32 or bfloat16, row (b, j) at element (b*N+j)*row_stride
+ * draft_q       [B, N, V] float32 contiguous: row j is what node j's children were drawn from
+ *               (rows of leaves are not read; NULL iff N == 1)
+ * draft_tokens, parents, uniforms   see above
+ * uniforms_rs   [B] float32 in [0,1): u'
+ * accept_len    [B] int32 out: accepted drafted tokens
+ * path          [B, N] int32 out: the root and the accepted nodes in order, then -1
+ * token         [B] int32 out
+ * edge_flags, rs_flags   [B] uint32 out, optional: DSSD_EDGE_FLAG_* of the rows and tokens that were looked at (BAD_PARENT: of
+ *               the whole tree), DSSD_RS_FLAG_* (BONUS: the token was drawn from p because the node has no child)
+ * workspace     >= dssd_tree_verify_workspace_bytes(B, N, V) bytes, 256-byte aligned
+ */
+dssd_status dssd_tree_verify(const void *target_logits, dssd_dtype dtype, int64_t row_stride, const float *draft_q,
+                             const int32_t *draft_tokens, const int32_t *parents, const float *uniforms,
+                             const float *uniforms_rs, float temperature, int replacement, int B, int N, int V,
+                             int32_t *accept_len, int32_t *path, int32_t *token, uint32_t *edge_flags,
+                             uint32_t *rs_flags, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Keys and values of accepted nodes into the pages, for all layers at once: rows path[b, 0 .. accept_len[b]] of
+ * sequence b go to positions ctx_len[b] .. ctx_len[b] + accept_len[b] (path == NULL: rows 0, 1, ...: a chain, or the
+ * tokens of a prompt).  accept_len[b] < 0 appends nothing.
+ *
+ * k_new, v_new  [layers, B, N, Hkv, D] of a 16-bit type, unit stride along D; new_strides (host): elements between layers,
+ *               sequences, nodes and heads
+ * k_cache, v_cache   [layers, num_pages, page_size, Hkv, D]; cache_strides (host): elements between layers, pages, positions and heads
+ * block_table, ctx_len   as for dssd_tree_attention
+ * path          [B, N] int32 or NULL
+ * new_len       [B] int32 out, optional: ctx_len + accept_len + 1 (+ N at most).  Not ctx_len itself (DSSD_ERR_INVALID_ARG)
+ * flags         [B] uint32 out, optional
+ * Two rows must not go to the same place; accept_len + 1 rows beyond N are left out (BAD_NODE).
+ */
+dssd_status dssd_cache_append(const void *k_new, const void *v_new, const int64_t *new_strides, void *k_cache,
+                              void *v_cache, const int64_t *cache_strides, dssd_dtype dtype,
+                              const int32_t *block_table, int64_t table_stride, int max_pages, int num_pages,
+                              int page_size, const int32_t *ctx_len, const int32_t *accept_len, const int32_t *path,
+                              int layers, int B, int N, int Hkv, int D, int32_t *new_len, uint32_t *flags,
+                              void *cuda_stream);
 
 #ifdef __cplusplus
 }

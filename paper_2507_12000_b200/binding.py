@@ -24,14 +24,25 @@ DSSD_ERR_WORKSPACE = 3
 DSSD_ERR_CUDA = 4
 DSSD_F32 = 0
 DSSD_BF16 = 1
+DSSD_F16 = 2
 
 EDGE_FLAG_BAD_TOKEN = 1
 EDGE_FLAG_NONFINITE = 2
 EDGE_FLAG_TIMEOUT = 4
+EDGE_FLAG_BAD_PARENT = 8
 RS_FLAG_BONUS = 1
 RS_FLAG_FALLBACK = 2
 RS_FLAG_INVALID = 4
 RS_FLAG_TIMEOUT = 8
+ADJUST_FLAG_BAD_TOKEN = 1
+ADJUST_FLAG_BAD_PARENT = 2
+ADJUST_FLAG_BAD_LENGTH = 4
+ADJUST_FLAG_BAD_VALUE = 8
+ADJUST_FLAG_BAD_MASK = 16
+CACHE_FLAG_BAD_PAGE = 1
+CACHE_FLAG_BAD_LENGTH = 2
+CACHE_FLAG_BAD_NODE = 4
+TREE_MAX_NODES = 128
 
 
 class DssdError(RuntimeError):
@@ -138,6 +149,20 @@ def _load(path: Optional[str] = None) -> ctypes.CDLL:
         c.c_void_p, c.c_int, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_float,
         c.c_int, c.c_int, c.c_int, c.c_int, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p,
         c.c_void_p, c.c_size_t, c.c_void_p]
+    i, p, i64 = c.c_int, c.c_void_p, c.c_int64
+    L.dssd_adjust_logits.restype = i
+    L.dssd_adjust_logits.argtypes = [p, i, i64, i, i, i, p, p, p, i64, i, p, p, p, p, p, p, p, i, p, i, p, p, i64, p, p]
+    L.dssd_tree_attention_workspace_bytes.restype = c.c_size_t
+    L.dssd_tree_attention_workspace_bytes.argtypes = [i, i, i, i, i]
+    L.dssd_tree_attention.restype = i
+    L.dssd_tree_attention.argtypes = [p, p, p, p, p, p, p, p, i, p, i64, i, i, i, p, p, i, i, i, i, i, c.c_float, p, p, p, p, p,
+                                      c.c_size_t, p]
+    L.dssd_tree_verify_workspace_bytes.restype = c.c_size_t
+    L.dssd_tree_verify_workspace_bytes.argtypes = [i, i, i]
+    L.dssd_tree_verify.restype = i
+    L.dssd_tree_verify.argtypes = [p, i, i64, p, p, p, p, p, c.c_float, i, i, i, i, p, p, p, p, p, p, c.c_size_t, p]
+    L.dssd_cache_append.restype = i
+    L.dssd_cache_append.argtypes = [p, p, p, p, p, p, i, p, i64, i, i, i, p, p, p, i, i, i, i, i, p, p, p]
     return L
 
 
@@ -494,4 +519,92 @@ def dssd_resample_shard_draw(masses: torch.Tensor, g: int, v_begin: int, p_row_s
                                       out, stream)
     if st != DSSD_OK:
         raise DssdError(st, "dssd_resample_shard_draw")
+    return out
+
+# ---- the round on a drafted tree ------------------------------------------------------------------
+
+
+def dssd_adjust_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = None, prompt_len: Optional[torch.Tensor] = None,
+                       history_len: Optional[torch.Tensor] = None, *, draft_tokens: Optional[torch.Tensor] = None,
+                       parents: Optional[torch.Tensor] = None, repetition: Optional[torch.Tensor] = None,
+                       presence: Optional[torch.Tensor] = None, frequency: Optional[torch.Tensor] = None,
+                       bias_tokens: Optional[torch.Tensor] = None, bias_values: Optional[torch.Tensor] = None,
+                       mask: Optional[torch.Tensor] = None, mask_row: Optional[torch.Tensor] = None,
+                       out: Optional[Dict[str, torch.Tensor]] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """Penalties, biases and masks on the logits [B, N, V] of N nodes (a chain's gamma+1 positions where parents is None).
+    Row j counts the history and the tokens drafted on its own way from the root.  mask: int32 words [rows, (V+31)//32], a set bit allows
+    its token; mask_row [B, N] names each row's mask (negative: none).  Returns {"logits", "flags"}; pass
+    out={"logits": logits, ...} to work in place."""
+    if out is None:
+        out = {"logits": torch.zeros_like(logits, memory_format=torch.contiguous_format),
+               "flags": torch.empty(logits.shape[0], dtype=torch.int32, device=logits.device)}
+    st = _marshal.adjust_logits(logits, history, prompt_len, history_len, draft_tokens, parents, repetition, presence, frequency,
+                                bias_tokens, bias_values, mask, mask_row, out, stream)
+    if st != DSSD_OK:
+        raise DssdError(st, "dssd_adjust_logits")
+    return out
+
+
+def dssd_tree_attention_workspace_bytes(B: int, N: int, Hq: int, Hkv: int, D: int) -> int:
+    return int(lib.dssd_tree_attention_workspace_bytes(B, N, Hq, Hkv, D))
+
+
+def dssd_tree_attention(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                        block_table: torch.Tensor, ctx_len: torch.Tensor, *, parents: Optional[torch.Tensor] = None,
+                        scale: Optional[float] = None, out: Optional[Dict[str, torch.Tensor]] = None, want_lse: bool = False,
+                        workspace: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """Attention of a drafted tree's nodes over a paged cache.  q [B, N, Hq, D]; k_new, v_new [B, N, Hkv, D]: the nodes' own keys
+    and values, not in the cache yet; k_cache, v_cache [pages, page_size, Hkv, D]; block_table [B, pages]; ctx_len
+    [B].  Returns {"o", "flags"} and, if asked, "lse" [B, N, Hq].  flags are added to what out["flags"] holds.  scale
+    defaults to 1/sqrt(D)."""
+    B, N, Hq, D = q.shape
+    if out is None:
+        out = {"o": torch.zeros_like(q, memory_format=torch.contiguous_format),
+               "flags": torch.zeros(B, dtype=torch.int32, device=q.device),
+               "lse": torch.zeros(B, N, Hq, dtype=torch.float32, device=q.device) if want_lse else None}
+    if workspace is None:
+        workspace = _workspace(dssd_tree_attention_workspace_bytes(B, N, Hq, k_new.shape[2], D), q.device)
+    st = _marshal.tree_attention(q, k_new, v_new, k_cache, v_cache, block_table, ctx_len, parents,
+                                 D ** -0.5 if scale is None else scale, out, workspace, stream)
+    if st != DSSD_OK:
+        raise DssdError(st, "dssd_tree_attention")
+    return out
+
+
+def dssd_tree_verify_workspace_bytes(B: int, N: int, V: int) -> int:
+    return int(lib.dssd_tree_verify_workspace_bytes(B, N, V))
+
+
+def dssd_tree_verify(target_logits: torch.Tensor, draft_q: Optional[torch.Tensor], draft_tokens: Optional[torch.Tensor],
+                     parents: Optional[torch.Tensor], uniforms: Optional[torch.Tensor], uniforms_rs: torch.Tensor,
+                     temperature: float, *, replacement: bool = True, out: Optional[Dict[str, torch.Tensor]] = None,
+                     workspace: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """The verdict on a drafted tree.  target_logits and draft_q [B, N, V] by node (row j of draft_q: what node j's children
+    were drawn from, with or without replacement); draft_tokens, parents, uniforms [B, N-1] for nodes 1 .. N-1.
+    Returns accept_len [B], path [B, N] (accepted nodes from the root on, then -1), token [B], edge_flags, rs_flags."""
+    B, g, V, dev = _sizes(target_logits)
+    if out is None:
+        out = {k: torch.empty(B, dtype=torch.int32, device=dev) for k in ("accept_len", "token", "edge_flags", "rs_flags")}
+        out["path"] = torch.empty(B, g + 1, dtype=torch.int32, device=dev)
+    if workspace is None:
+        workspace = _workspace(dssd_tree_verify_workspace_bytes(B, g + 1, V), dev)
+    st = _marshal.tree_verify(target_logits, draft_q, draft_tokens, parents, uniforms, uniforms_rs, temperature, replacement, out,
+                              workspace, stream)
+    if st != DSSD_OK:
+        raise DssdError(st, "dssd_tree_verify")
+    return out
+
+
+def dssd_cache_append(k_new: torch.Tensor, v_new: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                      block_table: torch.Tensor, ctx_len: torch.Tensor, accept_len: torch.Tensor, *,
+                      path: Optional[torch.Tensor] = None, out: Optional[Dict[str, torch.Tensor]] = None,
+                      stream=None) -> Dict[str, torch.Tensor]:
+    """Rows path[b, 0 .. accept_len[b]] of k_new, v_new [layers, B, N, Hkv, D] into the pages of k_cache, v_cache
+    [layers, pages, page_size, Hkv, D] from position ctx_len[b] on (path None: rows 0, 1, ...).  Returns {"new_len", "flags"}."""
+    if out is None:
+        B, dev = k_new.shape[1], k_new.device
+        out = {"new_len": torch.empty(B, dtype=torch.int32, device=dev), "flags": torch.empty(B, dtype=torch.int32, device=dev)}
+    st = _marshal.cache_append(k_new, v_new, k_cache, v_cache, block_table, ctx_len, accept_len, path, out, stream)
+    if st != DSSD_OK:
+        raise DssdError(st, "dssd_cache_append")
     return out

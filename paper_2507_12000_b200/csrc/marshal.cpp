@@ -11,6 +11,7 @@
 
 #include <vector>
 
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -24,7 +25,8 @@ namespace {
     X(dssd_device_resample_static) X(dssd_device_resample_rejected) X(dssd_edge_verify_topk)                  \
     X(dssd_device_resample_topk) X(dssd_dsd_verify) X(dssd_edge_verify_bonus) X(dssd_round_host)              \
     X(dssd_round_host_topk) X(dssd_edge_partial) X(dssd_edge_combine) X(dssd_edge_emit_shard)                 \
-    X(dssd_resample_shard_mass) X(dssd_resample_shard_draw)
+    X(dssd_resample_shard_mass) X(dssd_resample_shard_draw) X(dssd_adjust_logits) X(dssd_tree_attention)       \
+    X(dssd_tree_verify) X(dssd_cache_append)
 struct Calls {
 #define X(name) decltype(&::name) name;
     DSSD_CALLS(X)
@@ -447,6 +449,217 @@ dssd_status resample_shard_draw(PyObject *const *a)
                                         stream(a[10]));
 }
 
+// ---- the round on a drafted tree ---------------------------------------------------------------
+
+// Every tensor of a call is on one device, which is made the current one: a call on another device's tensors goes to that
+// device's current stream.
+struct OnDevice {
+    explicit OnDevice(const at::Tensor &t) : device(t.device()), guard(device) {}
+    const at::Device device;
+    const c10::cuda::CUDAGuard guard;
+};
+
+// a contiguous tensor of n values of one type on the call's device; None (or, with no values, anything) is NULL
+template <class T>
+T *values(const OnDevice &on, PyObject *o, at::ScalarType type, int64_t n, const char *what)
+{
+    if (o == nullptr || o == Py_None) return nullptr;
+    const at::Tensor &t = tensor(o);
+    require(t.numel() == n, what);
+    if (n == 0) return nullptr;
+    require(t.is_cuda() && t.device() == on.device && t.scalar_type() == type && t.is_contiguous(), what);
+    return static_cast<T *>(t.data_ptr());
+}
+template <class T>
+T *out_values(const OnDevice &on, PyObject *out, const char *name, at::ScalarType type, int64_t n, bool optional = false)
+{
+    PyObject *o;
+    if (!optional) o = item(out, name);
+    else o = PyDict_CheckExact(out) ? PyDict_GetItemString(out, name) : keep(PyObject_CallMethod(out, "get", "s", name));
+    if (optional && (o == nullptr || o == Py_None)) return nullptr;
+    require(o != Py_None, name);
+    return values<T>(on, o, type, n, name);
+}
+
+const at::Tensor &cuda_tensor(PyObject *o, int64_t dim, const char *what)
+{
+    const at::Tensor &t = tensor(o);
+    require(t.is_cuda() && t.dim() == dim, what);
+    return t;
+}
+
+int count(int64_t n)
+{
+    require(n <= 0x7fffffff, "a size of the call does not fit an int");
+    return (int)n;
+}
+
+// rows of history or of the block table: [B, n] int32 with unit stride; elements between rows
+struct Table {
+    const int32_t *data;
+    int64_t stride;
+    int n;
+};
+Table table(const OnDevice &on, PyObject *o, int64_t B, const char *what)
+{
+    const at::Tensor &t = tensor(o);
+    require(t.is_cuda() && t.device() == on.device && t.dim() == 2 && t.size(0) == B && t.scalar_type() == at::kInt &&
+                (t.stride(1) == 1 || t.size(1) <= 1), what);
+    const int64_t stride = B > 1 ? t.stride(0) : t.size(1);
+    require(stride >= t.size(1), what);
+    return {t.numel() ? static_cast<const int32_t *>(t.data_ptr()) : nullptr, stride, count(t.size(1))};
+}
+
+// logits, history, prompt_len, history_len, draft_tokens, parents, repetition, presence, frequency, bias_tokens, bias_values,
+// mask, mask_row, out, stream
+dssd_status adjust_logits(PyObject *const *a)
+{
+    const Rows r = rows(a[0]);
+    const at::Tensor &in = tensor(a[0]);
+    const OnDevice on(in);
+    const int64_t B = r.B, N = r.gamma + 1, nodes = B * (N - 1);
+    const at::Tensor &o = tensor(item(a[13], "logits"));
+    require(o.is_cuda() && o.device() == on.device && o.sizes() == in.sizes() && o.scalar_type() == in.scalar_type() &&
+                (o.stride(2) == 1 || o.size(2) == 1), "out[\"logits\"] must be like logits");
+    const int64_t o_stride = row_stride(o, "rows of out[\"logits\"] must be equally spaced");
+    require(r.stride >= r.V && o_stride >= r.V, "rows of the logits must not overlap");
+    Table h{nullptr, 0, 0};
+    if (a[1] != Py_None) h = table(on, a[1], B, "history must be an int32 [B, L] tensor with unit stride along L");
+    const int32_t *pl = values<const int32_t>(on, a[2], at::kInt, B, "prompt_len must be an int32 [B] tensor");
+    const int32_t *hl = values<const int32_t>(on, a[3], at::kInt, B, "history_len must be an int32 [B] tensor");
+    const int32_t *tok = values<const int32_t>(on, a[4], at::kInt, nodes, "draft_tokens must be an int32 [B, N-1] tensor");
+    const int32_t *par = values<const int32_t>(on, a[5], at::kInt, nodes, "parents must be an int32 [B, N-1] tensor");
+    const float *rep = values<const float>(on, a[6], at::kFloat, B, "repetition must be a float32 [B] tensor");
+    const float *pre = values<const float>(on, a[7], at::kFloat, B, "presence must be a float32 [B] tensor");
+    const float *fre = values<const float>(on, a[8], at::kFloat, B, "frequency must be a float32 [B] tensor");
+    int K = 0;
+    const int32_t *bt = nullptr;
+    const float *bv = nullptr;
+    if (a[9] != Py_None) {
+        const at::Tensor &t = cuda_tensor(a[9], 2, "bias_tokens must be an int32 [B, K] tensor");
+        K = count(t.size(1));
+        bt = values<const int32_t>(on, a[9], at::kInt, B * K, "bias_tokens must be an int32 [B, K] tensor");
+        bv = values<const float>(on, a[10], at::kFloat, B * K, "bias_values must be a float32 [B, K] tensor");
+    }
+    int mask_rows = 0;
+    const uint32_t *mask = nullptr;
+    const int32_t *mask_row = nullptr;
+    if (a[11] != Py_None) {
+        const at::Tensor &t = cuda_tensor(a[11], 2, "mask must be an int32 [rows, (V+31)/32] tensor");
+        require(t.size(1) == (r.V + 31) / 32, "mask must be an int32 [rows, (V+31)/32] tensor");
+        mask_rows = count(t.size(0));
+        mask = values<const uint32_t>(on, a[11], at::kInt, t.numel(), "mask must be an int32 [rows, (V+31)/32] tensor");
+        mask_row = values<const int32_t>(on, a[12], at::kInt, B * N, "mask_row must be an int32 [B, N] tensor");
+    }
+    uint32_t *fl = out_values<uint32_t>(on, a[13], "flags", at::kInt, B, true);
+    void *s = stream(a[14]);
+    return call(lib.dssd_adjust_logits, r.data, r.dtype, r.stride, r.B, (int)N, r.V, tok, par, h.data, h.stride, h.n, pl, hl, rep, pre, fre,
+                bt, bv, K, mask, mask_rows, mask_row, o.data_ptr(), o_stride, fl, s);
+}
+
+dssd_dtype half_code(const at::Tensor &t)
+{
+    if (t.scalar_type() == at::kBFloat16) return DSSD_BF16;
+    if (t.scalar_type() == at::kHalf) return DSSD_F16;
+    raise(PyExc_TypeError, "keys and values must be bfloat16 or float16");
+}
+
+// strides of all dimensions but the last, in elements; those of dimensions of one entry do not matter
+struct Strides {
+    int64_t s[4];
+};
+Strides strides(const at::Tensor &t, const char *what)
+{
+    const int64_t n = t.dim();
+    require(t.stride(n - 1) == 1 || t.size(n - 1) == 1, what);
+    Strides r{};
+    for (int64_t i = 0; i < n - 1; ++i) r.s[i] = t.size(i) > 1 ? t.stride(i) : 0;
+    return r;
+}
+// two tensors of one type, shape and spacing on the call's device
+void alike(const OnDevice &on, const at::Tensor &k, const at::Tensor &v, const char *what)
+{
+    require(k.is_cuda() && k.device() == on.device && v.is_cuda() && v.device() == on.device && k.sizes() == v.sizes() &&
+                k.scalar_type() == v.scalar_type() && k.strides() == v.strides(), what);
+}
+
+// q, k_new, v_new, k_cache, v_cache, block_table, ctx_len, parents, scale, out, workspace, stream
+dssd_status tree_attention(PyObject *const *a)
+{
+    const at::Tensor &q = cuda_tensor(a[0], 4, "q must be a [B, N, Hq, D] CUDA tensor");
+    const OnDevice on(q);
+    const at::Tensor &kn = cuda_tensor(a[1], 4, "k_new must be a [B, N, Hkv, D] CUDA tensor"), &vn = tensor(a[2]);
+    const at::Tensor &kc = cuda_tensor(a[3], 4, "k_cache must be a [pages, page_size, Hkv, D] CUDA tensor"), &vc = tensor(a[4]);
+    alike(on, kn, vn, "v_new must be like k_new");
+    alike(on, kc, vc, "v_cache must be like k_cache");
+    const int64_t B = q.size(0), N = q.size(1), Hq = q.size(2), D = q.size(3), Hkv = kn.size(2);
+    require(kn.size(0) == B && kn.size(1) == N && kn.size(3) == D && kc.size(2) == Hkv && kc.size(3) == D && kn.scalar_type() == q.scalar_type() &&
+                kc.scalar_type() == q.scalar_type(), "q, k_new and k_cache must have the same sequences, nodes, heads, head size and type");
+    const at::Tensor &o = tensor(item(a[9], "o"));
+    require(o.is_cuda() && o.device() == on.device && o.sizes() == q.sizes() && o.scalar_type() == q.scalar_type(), "out[\"o\"] must be like q");
+    const Strides sq = strides(q, "q must have unit stride along D"), sn = strides(kn, "k_new must have unit stride along D"),
+                  sc = strides(kc, "k_cache must have unit stride along D"), so = strides(o, "out[\"o\"] must have unit stride along D");
+    const Table bt = table(on, a[5], B, "block_table must be an int32 [B, pages] tensor with unit stride along the pages");
+    const int32_t *len = values<const int32_t>(on, a[6], at::kInt, B, "ctx_len must be an int32 [B] tensor");
+    const int32_t *par = values<const int32_t>(on, a[7], at::kInt, B * (N - 1), "parents must be an int32 [B, N-1] tensor");
+    const float scale = (float)number(a[8]);
+    float *lse = out_values<float>(on, a[9], "lse", at::kFloat, B * N * Hq, true);
+    uint32_t *fl = out_values<uint32_t>(on, a[9], "flags", at::kInt, B, true);
+    const Space ws = space(a[10]);
+    require(tensor(a[10]).device() == on.device, "the workspace must be on the same device");
+    void *s = stream(a[11]);
+    return call(lib.dssd_tree_attention, q.data_ptr(), sq.s, kn.data_ptr(), vn.data_ptr(), sn.s, kc.data_ptr(), vc.data_ptr(), sc.s,
+                half_code(q), bt.data, bt.stride, bt.n, count(kc.size(0)), count(kc.size(1)), len, par, count(B), count(N), count(Hq), count(Hkv),
+                count(D), scale, o.data_ptr(), so.s, lse, fl, ws.data, ws.bytes, s);
+}
+
+// target_logits, draft_q, draft_tokens, parents, uniforms, uniforms_rs, temperature, replacement, out, workspace, stream
+dssd_status tree_verify(PyObject *const *a)
+{
+    const Rows r = rows(a[0]);
+    const OnDevice on(tensor(a[0]));
+    const int64_t B = r.B, N = r.gamma + 1, nodes = B * (N - 1);
+    require(r.stride >= r.V, "rows of target_logits must not overlap");
+    const float *q = N > 1 ? values<const float>(on, a[1], at::kFloat, B * N * r.V, "draft_q must be a contiguous float32 [B, N, V] tensor") : nullptr;
+    const int32_t *tok = values<const int32_t>(on, a[2], at::kInt, nodes, "draft_tokens must be an int32 [B, N-1] tensor");
+    const int32_t *par = values<const int32_t>(on, a[3], at::kInt, nodes, "parents must be an int32 [B, N-1] tensor");
+    const float *u = values<const float>(on, a[4], at::kFloat, nodes, "uniforms must be a float32 [B, N-1] tensor");
+    const float *ur = values<const float>(on, a[5], at::kFloat, B, "uniforms_rs must be a float32 [B] tensor");
+    const float T = (float)number(a[6]);
+    const int with = PyObject_IsTrue(a[7]);
+    int32_t *n = out_values<int32_t>(on, a[8], "accept_len", at::kInt, B), *path = out_values<int32_t>(on, a[8], "path", at::kInt, B * N);
+    int32_t *token = out_values<int32_t>(on, a[8], "token", at::kInt, B);
+    uint32_t *ef = out_values<uint32_t>(on, a[8], "edge_flags", at::kInt, B, true), *rf = out_values<uint32_t>(on, a[8], "rs_flags", at::kInt, B, true);
+    const Space ws = space(a[9]);
+    require(tensor(a[9]).device() == on.device, "the workspace must be on the same device");
+    void *s = stream(a[10]);
+    return call(lib.dssd_tree_verify, r.data, r.dtype, r.stride, q, tok, par, u, ur, T, with == 1 ? 1 : 0, r.B, (int)N, r.V, n, path, token, ef, rf,
+                ws.data, ws.bytes, s);
+}
+
+// k_new, v_new, k_cache, v_cache, block_table, ctx_len, accept_len, path, out, stream
+dssd_status cache_append(PyObject *const *a)
+{
+    const at::Tensor &kn = cuda_tensor(a[0], 5, "k_new must be a [layers, B, N, Hkv, D] CUDA tensor"), &vn = tensor(a[1]);
+    const OnDevice on(kn);
+    const at::Tensor &kc = cuda_tensor(a[2], 5, "k_cache must be a [layers, pages, page_size, Hkv, D] CUDA tensor"), &vc = tensor(a[3]);
+    alike(on, kn, vn, "v_new must be like k_new");
+    alike(on, kc, vc, "v_cache must be like k_cache");
+    const int64_t L = kn.size(0), B = kn.size(1), N = kn.size(2), Hkv = kn.size(3), D = kn.size(4);
+    require(kc.size(0) == L && kc.size(3) == Hkv && kc.size(4) == D && kc.scalar_type() == kn.scalar_type(),
+            "k_new and k_cache must have the same layers, heads, head size and type");
+    const Strides sn = strides(kn, "k_new must have unit stride along D"), sc = strides(kc, "k_cache must have unit stride along D");
+    const Table bt = table(on, a[4], B, "block_table must be an int32 [B, pages] tensor with unit stride along the pages");
+    const int32_t *len = values<const int32_t>(on, a[5], at::kInt, B, "ctx_len must be an int32 [B] tensor");
+    const int32_t *acc = values<const int32_t>(on, a[6], at::kInt, B, "accept_len must be an int32 [B] tensor");
+    const int32_t *path = values<const int32_t>(on, a[7], at::kInt, B * N, "path must be an int32 [B, N] tensor");
+    int32_t *nl = out_values<int32_t>(on, a[8], "new_len", at::kInt, B, true);
+    uint32_t *fl = out_values<uint32_t>(on, a[8], "flags", at::kInt, B, true);
+    void *s = stream(a[9]);
+    return call(lib.dssd_cache_append, kn.data_ptr(), vn.data_ptr(), sn.s, kc.data_ptr(), vc.data_ptr(), sc.s, half_code(kn), bt.data, bt.stride,
+                bt.n, count(kc.size(1)), count(kc.size(2)), len, acc, path, count(L), count(B), count(N), count(Hkv), count(D), nl, fl, s);
+}
+
 // ---- glue -----------------------------------------------------------------------------------
 
 template <dssd_status (*fn)(PyObject *const *), Py_ssize_t kArgs>
@@ -511,6 +724,10 @@ PyMethodDef methods[] = {
     ENTRY(edge_emit_shard, 6),
     ENTRY(resample_shard_mass, 7),
     ENTRY(resample_shard_draw, 11),
+    ENTRY(adjust_logits, 15),
+    ENTRY(tree_attention, 12),
+    ENTRY(tree_verify, 11),
+    ENTRY(cache_append, 10),
     {nullptr, nullptr, 0, nullptr},
 };
 

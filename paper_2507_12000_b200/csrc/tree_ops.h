@@ -1,0 +1,81 @@
+// Host-side interface of the kernels of a round on a drafted tree (internal to the library).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace dssd {
+
+struct AdjustParams {
+    const void *logits;
+    void *out;
+    int64_t row_stride, out_stride;
+    const int32_t *draft_tokens, *parents;
+    const int32_t *history;
+    int64_t history_stride;
+    const int32_t *prompt_len, *history_len;
+    const float *repetition, *presence, *frequency;
+    const int32_t *bias_tokens;
+    const float *bias_values;
+    const uint32_t *mask;
+    const int32_t *mask_row;
+    uint32_t *flags;
+    int B, N, V, L, K, mask_rows;
+    // geometry
+    int slices;        // CTAs per sequence, a slice of the vocabulary each
+    int slice;         // entries of a slice, a multiple of 1024
+    int segments;      // pieces of 1024 entries that a row's slice touches
+};
+cudaError_t adjust_launch(AdjustParams &P, int dtype, cudaStream_t stream);
+
+struct TreeVerifyParams {
+    const void *logits;
+    int64_t row_stride;
+    const float *draft_q;
+    const int32_t *draft_tokens, *parents;
+    const float *uniforms, *uniforms_rs;
+    double c1;  // log2(e) / T
+    int replacement, B, N, V;
+    int32_t *accept_len, *path, *token;
+    uint32_t *edge_flags, *rs_flags;
+    int slice;  // entries of the vocabulary per CTA of the sequence's cluster
+};
+size_t tree_verify_workspace(int B, int N, int V);
+cudaError_t tree_verify_launch(TreeVerifyParams &P, int dtype, void *workspace, cudaStream_t stream);
+
+struct AppendParams {
+    const void *k_new, *v_new;
+    void *k_cache, *v_cache;
+    int64_t new_l, new_b, new_n, new_h;          // strides in elements
+    int64_t cache_l, cache_p, cache_t, cache_h;
+    const int32_t *block_table;
+    int64_t table_stride;
+    int max_pages, num_pages, page_size;
+    const int32_t *ctx_len, *accept_len, *path;
+    int layers, B, N, Hkv, D;
+    int32_t *new_len;
+    uint32_t *flags;
+};
+cudaError_t append_launch(AppendParams &P, cudaStream_t stream);
+
+struct TreeAttentionParams {
+    const void *q, *k_new, *v_new, *k_cache, *v_cache;
+    int64_t q_b, q_n, q_h;                        // strides in elements
+    int64_t new_b, new_n, new_h;
+    int64_t cache_p, cache_t, cache_h;
+    int64_t o_b, o_n, o_h;
+    const int32_t *block_table;
+    int64_t table_stride;
+    int max_pages, num_pages, page_size;
+    const int32_t *ctx_len, *parents;
+    int B, N, Hq, Hkv, D;
+    float scale;
+    void *o;
+    float *lse;
+    uint32_t *flags;
+};
+size_t tree_attention_workspace(int B, int N, int Hq, int Hkv, int D);
+cudaError_t tree_attention_launch(TreeAttentionParams &P, int dtype, void *workspace, cudaStream_t stream);
+
+}  // namespace dssd
