@@ -42,6 +42,7 @@ ADJUST_FLAG_BAD_MASK = 16
 CACHE_FLAG_BAD_PAGE = 1
 CACHE_FLAG_BAD_LENGTH = 2
 CACHE_FLAG_BAD_NODE = 4
+CACHE_FLAG_TIMEOUT = 8
 TREE_MAX_NODES = 128
 
 

@@ -1,9 +1,24 @@
 // Attention of a drafted tree's nodes over a paged cache.
 //
-// The plain kernel: a CTA per (sequence, node, query head), a warp per key in turn, lanes along D, a running maximum and sum per
-// warp, joined at the end.
+// The rows of a key head are the nodes times the query heads that share it, 128 to a tile of the tensor core: S = Q K^T for 128
+// keys at a time into tensor memory, a thread per row for the softmax, P back into tensor memory as 16-bit values, O += P V.  A tile of
+// keys serves all rows of its head, so the cache is read once (once per 256 rows).  The keys of a sequence are
+// its nodes (tile 0, masked by ancestors) and then the cache, 128 positions to a tile, brought in by tiled copies, one per page or part of a
+// page, into a ring of stages; the copies fill what lies outside a head's size with zeros, so any size works on 64 or 128 columns.
+//
+// What bounds it: the cache's bytes as long as a tile's 64 KB take longer to arrive (2900 cycles of an SM's share of the measured
+// bandwidth) than 128 rows of softmax (128 exponentials a thread, 1024 cycles of the special-function units) and
+// two products (1024 cycles); for 256 rows the products and exponentials come to the same 2048 cycles.
+//
+// Split: all (sequence, key head, row tile) items, each with its tiles, lie on one line, and every CTA takes an equal piece of that line whatever the lengths are.
+// An item that lies in several pieces leaves a partial result (O, maximum, sum) per piece in the workspace, at places that only its CTA writes, and a second
+// kernel joins them in order: the same bits on every run, and nothing to clear.
+//
+// The maximum that weights refer to is only raised when a tile exceeds it by more than 2^8: raising it means to read, scale and write back O.
+// The sum refers to the same maximum, so the quotient is not changed; P stays below 2^8.
 #include "launch.h"
 #include "quads.cuh"
+#include "tcgen05.cuh"
 #include "tree.cuh"
 #include "tree_ops.h"
 
@@ -13,100 +28,725 @@ namespace dssd {
 
 namespace {
 
-template <int DT>
-__device__ __forceinline__ float value(const void *p, int64_t i)
+constexpr int kTile = 128;      // keys of a tile, rows of a tile
+constexpr int kMaxCtas = 148;   // pieces of the line
+constexpr int kMinTiles = 2;    // tiles to a piece at least
+constexpr int kThreadsOf[3] = {0, 256, 384};
+
+struct Geometry {
+    CUtensorMap q, k_new, v_new, k_cache, v_cache;
+    const int32_t *block_table;
+    int64_t table_stride;
+    int max_pages, num_pages, page_size, box;  // box: positions of a copy, the greatest common divisor of the page and 128
+    const int32_t *ctx_len, *parents;
+    int B, N, Hkv, G, D;
+    int nodes_per_tile, row_items;  // nodes in a tile of rows; items of kMT tiles to a key head
+    float scale, c;                 // c = scale * log2(e)
+    void *o;
+    int64_t o_b, o_n, o_h;
+    float *lse;
+    uint32_t *flags;
+    float *part;     // [2 kMaxCtas][kMT * 128][kDP]
+    float2 *part_ml; // [2 kMaxCtas][kMT * 128] maximum in powers of two, sum
+};
+
+__device__ __forceinline__ int length(const Geometry &P, long long b, bool *bad = nullptr)
 {
-    const uint32_t h = ld_row_u16(static_cast<const char *>(p) + 2 * i);
-    return DT == DSSD_BF16 ? __uint_as_float(h << 16) : __half2float(__ushort_as_half((unsigned short)h));
+    const int n = ld_after(P.ctx_len + b);
+    const int most = P.max_pages * P.page_size;
+    if (bad) *bad = n < 0 || n > most;
+    return min(max(n, 0), most);
 }
-template <int DT>
-__device__ __forceinline__ unsigned short bits(float x)
+__device__ __forceinline__ int tiles_of(int ctx) { return 1 + (ctx + kTile - 1) / kTile; }
+
+// all tiles of the line, and of the sequences before b, by one warp (all lanes get both)
+struct Line {
+    long long total, before;
+};
+__device__ Line measure(const Geometry &P, long long b, bool report)
 {
-    return DT == DSSD_BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : __half_as_ushort(__float2half_rn(x));
+    const int lane = threadIdx.x & 31;
+    long long all = 0, before = 0;
+    for (long long i = lane; i < P.B; i += 32) {
+        bool bad;
+        const int t = tiles_of(length(P, i, &bad));
+        if (report && bad && P.flags) atomicOr(P.flags + i, DSSD_CACHE_FLAG_BAD_LENGTH);
+        all += t;
+        if (i < b) before += t;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        all += __shfl_xor_sync(0xffffffffu, all, o);
+        before += __shfl_xor_sync(0xffffffffu, before, o);
+    }
+    const long long items = (long long)P.Hkv * P.row_items;
+    return {all * items, before * items};
+}
+__device__ __forceinline__ long long pieces(long long total, unsigned grid)
+{
+    const long long n = (total + kMinTiles - 1) / kMinTiles;
+    return n < (long long)grid ? n : (long long)grid;
 }
 
-constexpr int kAT = 128;
+// where a piece of the line begins
+struct Place {
+    long long b;
+    int item, tile, tiles;  // item of the sequence; tile of it; its tiles
+    int ctx;
+};
+__device__ Place find(const Geometry &P, long long at)  // one warp, all lanes get it
+{
+    const int lane = threadIdx.x & 31;
+    const long long items = (long long)P.Hkv * P.row_items;
+    Place r = {0, 0, 0, 1, 0};
+    long long base = 0;
+    for (long long i0 = 0; i0 < P.B; i0 += 32) {
+        const long long i = i0 + lane;
+        const int ctx = i < P.B ? length(P, i) : 0;
+        const int t = i < P.B ? tiles_of(ctx) : 0;
+        long long end = t;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long up = __shfl_up_sync(0xffffffffu, end, o);
+            if (lane >= o) end += up;
+        }
+        const unsigned in = __ballot_sync(0xffffffffu, i < P.B && base + end * items > at);
+        if (in) {
+            const int l = __ffs(in) - 1;
+            const long long start = base + (__shfl_sync(0xffffffffu, end, l) - __shfl_sync(0xffffffffu, t, l)) * items;
+            r.b = i0 + l;
+            r.tiles = __shfl_sync(0xffffffffu, t, l);
+            r.ctx = __shfl_sync(0xffffffffu, ctx, l);
+            r.item = (int)((at - start) / r.tiles);
+            r.tile = (int)((at - start) - (long long)r.item * r.tiles);
+            return r;
+        }
+        base += __shfl_sync(0xffffffffu, end, 31) * items;
+    }
+    return r;
+}
+// the next item
+__device__ __forceinline__ void advance(const Geometry &P, Place &p)
+{
+    p.tile = 0;
+    if (++p.item == P.Hkv * P.row_items) {
+        p.item = 0;
+        if (++p.b < P.B) {
+            p.ctx = length(P, p.b);
+            p.tiles = tiles_of(p.ctx);
+        }
+    }
+}
 
 template <int DT>
-__global__ void __launch_bounds__(kAT) plain_attention_kernel(const __grid_constant__ TreeAttentionParams P)
+__device__ __forceinline__ uint32_t pack(float lo, float hi)
 {
-    __shared__ short parent[kMaxNodes];
-    __shared__ int bad;
-    __shared__ float acc[4][128], top[4], sum[4];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int hq = blockIdx.x % (unsigned)P.Hq;
-    const int j = (blockIdx.x / (unsigned)P.Hq) % (unsigned)P.N;
-    const long long b = blockIdx.x / (unsigned)P.Hq / (unsigned)P.N;
-    const int h = hq / (P.Hq / P.Hkv);
+    if (DT == DSSD_BF16) {
+        uint32_t r;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
+    }
+    return pack_half2(lo, hi);
+}
+
+template <int DP, int kMT>
+struct Smem {
+    static constexpr int kStages = DP == 64 ? (kMT == 1 ? 6 : 5) : (kMT == 1 ? 3 : 2);
+    static constexpr int kChunk = kTile * 128;             // 64 columns of a tile
+    static constexpr int kOperand = kTile * DP * 2;
+    static constexpr int kQ = 0, kKV = kMT * kOperand;     // then K and V of the stages in turn
+    static constexpr int kRest = kKV + kStages * 2 * kOperand;
+    struct Rest {
+        uint64_t q_full, q_empty, k_full[kStages], v_full[kStages], k_empty[kStages], v_empty[kStages], s_full[2], p_ready[2], o_done[kMT], o_free[kMT];
+        short parent[4 * kMT][128];  // of the nodes, for each warp of the softmax
+        Place place;
+        long long count;
+        uint32_t tmem;
+        int failed;
+    };
+    static constexpr size_t kBytes = kRest + sizeof(Rest) + 1024;  // (the base is aligned by hand)
+    static_assert(kBytes <= 232448, "a CTA has 227 KB of shared memory");
+};
+
+template <int DT, int DP, int kMT>
+__global__ void __launch_bounds__(kThreadsOf[kMT], 1) tree_attention_kernel(const __grid_constant__ Geometry P)
+{
+    typedef Smem<DP, kMT> M;
+    extern __shared__ unsigned char raw[];
+    unsigned char *base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+    typename M::Rest &S = *reinterpret_cast<typename M::Rest *>(base + M::kRest);
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    constexpr int kChunks = DP / 64;
+
+    if (t == 0) {
+        bar_init(&S.q_full, 1);
+        bar_init(&S.q_empty, 1);
+        for (int i = 0; i < M::kStages; ++i) {
+            bar_init(&S.k_full[i], 1);
+            bar_init(&S.v_full[i], 1);
+            bar_init(&S.k_empty[i], 1);
+            bar_init(&S.v_empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(&S.s_full[i], 1);
+            bar_init(&S.p_ready[i], 128);
+        }
+        for (int i = 0; i < kMT; ++i) {
+            bar_init(&S.o_done[i], 1);
+            bar_init(&S.o_free[i], 128);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        S.failed = 0;
+    }
+    if (warp == 2) tmem_alloc(&S.tmem, 512);
+    if (warp == 0 && lane == 0) {
+        prefetch_map(&P.q);
+        prefetch_map(&P.k_new);
+        prefetch_map(&P.v_new);
+        prefetch_map(&P.k_cache);
+        prefetch_map(&P.v_cache);
+    }
     pdl_wait();
     pdl_trigger();
-    load_tree(P.parents, b, P.N, parent, &bad);
-    unsigned flags = bad ? DSSD_CACHE_FLAG_BAD_NODE : 0u;
-    const long long most = (long long)P.max_pages * P.page_size;
-    int ctx = ld_after(P.ctx_len + b);
-    if (ctx < 0 || ctx > most) {
-        ctx = ctx < 0 ? 0 : (int)most;
-        flags |= DSSD_CACHE_FLAG_BAD_LENGTH;
+    if (warp == 3) {  // which piece of the line is this CTA's
+        const long long total = measure(P, 0, blockIdx.x == 0).total;
+        const long long n = pieces(total, gridDim.x);
+        long long from = 0, to = 0;
+        if ((long long)blockIdx.x < n) from = blockIdx.x * total / n, to = (blockIdx.x + 1ll) * total / n;
+        Place p = {0, 0, 0, 1, 0};
+        if (to > from) p = find(P, from);
+        if (lane == 0) S.place = p, S.count = to - from;
     }
-    if (parent[j] >= 0) {
-        float q[4], o[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < 4; ++k) q[k] = lane + 32 * k < P.D ? value<DT>(P.q, b * P.q_b + j * P.q_n + hq * P.q_h + lane + 32 * k) * P.scale : 0.f;
-        float m = DSSD_NEG_INF, l = 0.f;
-        for (long long t = warp; t < (long long)ctx + P.N; t += 4) {
-            const void *kp = P.k_cache, *vp = P.v_cache;
-            int64_t at;
-            if (t < ctx) {
-                const int page = ld_after(P.block_table + b * P.table_stride + t / P.page_size);
-                if (page < 0 || page >= P.num_pages) flags |= DSSD_CACHE_FLAG_BAD_PAGE;
-                at = page < 0 || page >= P.num_pages ? -1 : page * P.cache_p + (t % P.page_size) * P.cache_t + h * P.cache_h;
-            } else {
-                const int i = (int)(t - ctx);
-                int up = j;
-                while (up > i) up = parent[up];
-                if (up != i) continue;
-                kp = P.k_new, vp = P.v_new;
-                at = b * P.new_b + i * P.new_n + h * P.new_h;
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = S.tmem;
+    volatile int *failed = &S.failed;
+    Place at = S.place;
+    long long left = S.count;
+
+    if (warp == 0) {
+        // ---- copies: every lane brings in boxes of its own
+        int stage = 0;
+        unsigned round = 0, items = 0;
+        bool ok = true;
+        while (left > 0 && ok) {
+            const int h = at.item / P.row_items, rt = at.item - h * P.row_items;
+            const int n = (int)(left < at.tiles - at.tile ? left : at.tiles - at.tile);
+            if (items) ok = warp_wait(&S.q_empty, (items - 1) & 1, failed);
+            if (ok && lane == 0) {
+                bar_expect(&S.q_full, (uint32_t)(kMT * kChunks * P.nodes_per_tile * P.G * 128));
+                for (int m = 0; m < kMT; ++m)
+                    for (int x = 0; x < kChunks; ++x)
+                        copy_5d(base + M::kQ + m * M::kOperand + x * M::kChunk, &P.q, &S.q_full, x * 64, 0, h, (rt * kMT + m) * P.nodes_per_tile, (int)at.b);
             }
-            float s = 0.f;
-            for (int k = 0; k < 4; ++k)
-                if (lane + 32 * k < P.D && at >= 0) s += q[k] * value<DT>(kp, at + lane + 32 * k);
-            s = warp_sum(s);
-            const float mn = fmaxf(m, s), w = expf(s - mn), f = expf(m - mn);
-            m = mn;
-            l = l * f + w;
-            for (int k = 0; k < 4; ++k) o[k] = o[k] * f + (lane + 32 * k < P.D && at >= 0 ? w * value<DT>(vp, at + lane + 32 * k) : 0.f);
+            ++items;
+            for (int i = at.tile; ok && i < at.tile + n; ++i) {
+                unsigned char *k = base + M::kKV + stage * 2 * M::kOperand, *v = k + M::kOperand;
+                const int pos = (i - 1) * kTile;
+                const int valid = i == 0 ? P.N : min(kTile, at.ctx - pos);
+                const int boxes = i == 0 ? 1 : (valid + P.box - 1) / P.box;
+                const uint32_t bytes = (uint32_t)(kChunks * 128 * (i == 0 ? P.N : boxes * P.box));
+                // the pages are looked up before the wait for the stage: two boxes to a lane, for pages of four and more
+                constexpr int kAhead = 2;
+                int page[kAhead], off[kAhead];
+                auto lookup = [&](int x, int &pg, int &of) {
+                    const int p = pos + (x % boxes) * P.box;
+                    of = p % P.page_size;
+                    pg = ld_after(P.block_table + at.b * P.table_stride + p / P.page_size);
+                    if (pg < 0 || pg >= P.num_pages) {
+                        if (P.flags) atomicOr(P.flags + at.b, DSSD_CACHE_FLAG_BAD_PAGE);
+                        pg = max(P.num_pages, 1);  // outside the cache: zeros come
+                    }
+                };
+                if (i > 0)
+#pragma unroll
+                    for (int a = 0; a < kAhead; ++a)
+                        if (lane + 32 * a < boxes * kChunks) lookup(lane + 32 * a, page[a], off[a]);
+                ok = warp_wait(&S.k_empty[stage], (round & 1) ^ 1, failed);
+                if (!ok) break;
+                if (lane == 0) bar_expect(&S.k_full[stage], bytes);
+                __syncwarp();
+                auto bring = [&](unsigned char *to, const CUtensorMap *fresh, const CUtensorMap *cache, uint64_t *bar) {
+                    if (i == 0) {
+                        if (lane < kChunks) copy_4d(to + lane * M::kChunk, fresh, bar, lane * 64, h, 0, (int)at.b);
+                        return;
+                    }
+#pragma unroll
+                    for (int a = 0; a < kAhead; ++a) {
+                        const int x = lane + 32 * a;
+                        if (x < boxes * kChunks) copy_4d(to + (x / boxes) * M::kChunk + (x % boxes) * P.box * 128, cache, bar, (x / boxes) * 64, h, off[a], page[a]);
+                    }
+                    for (int x = lane + 32 * kAhead; x < boxes * kChunks; x += 32) {
+                        int pg, of;
+                        lookup(x, pg, of);
+                        copy_4d(to + (x / boxes) * M::kChunk + (x % boxes) * P.box * 128, cache, bar, (x / boxes) * 64, h, of, pg);
+                    }
+                };
+                bring(k, &P.k_new, &P.k_cache, &S.k_full[stage]);
+                ok = warp_wait(&S.v_empty[stage], (round & 1) ^ 1, failed);
+                if (!ok) break;
+                if (lane == 0) bar_expect(&S.v_full[stage], bytes);
+                __syncwarp();
+                bring(v, &P.v_new, &P.v_cache, &S.v_full[stage]);
+                if (++stage == M::kStages) stage = 0, ++round;
+            }
+            left -= n;
+            advance(P, at);
         }
-        for (int k = 0; k < 4; ++k) acc[warp][lane + 32 * k] = o[k];
-        if (lane == 0) top[warp] = m, sum[warp] = l;
-        __syncthreads();
-        float mt = DSSD_NEG_INF, lt = 0.f, ot = 0.f;
-        for (int w = 0; w < 4; ++w) mt = fmaxf(mt, top[w]);
-        for (int w = 0; w < 4; ++w) {
-            const float f = top[w] == DSSD_NEG_INF ? 0.f : expf(top[w] - mt);
-            lt += f * sum[w];
-            ot += f * acc[w][threadIdx.x];
+    } else if (warp == 1) {
+        // ---- products, issued by one thread
+        if (lane == 0) {
+            int stage = 0, next = 0;  // of PV, of QK
+            unsigned round = 0, next_round = 0, items = 0;
+            unsigned p_phase[2] = {0, 0};
+            bool ok = true;
+            const uint32_t q0 = smem_u32(base + M::kQ), kv0 = smem_u32(base + M::kKV);
+            int sbuf = 0;  // (one tile of rows) the buffer of the next S
+            while (left > 0 && ok) {
+                const int n = (int)(left < at.tiles - at.tile ? left : at.tiles - at.tile);
+                ok = bar_wait(&S.q_full, items & 1, failed);
+                if (!ok) break;
+                auto valid_of = [&](int i) { return i == 0 ? P.N : min(kTile, at.ctx - (i - 1) * kTile); };
+                auto scores = [&](int m, int buf, int i) {
+                    const uint32_t k = kv0 + next * 2 * M::kOperand;
+                    const uint32_t sh = shape<DT == DSSD_BF16>(128, (valid_of(i) + 15) / 16 * 16, false);
+#pragma unroll
+                    for (int x = 0; x < DP / 16; ++x) {
+                        const uint32_t in = (x / 4) * M::kChunk + (x % 4) * 32;
+                        mma_ss(tmem + buf * 128, operand(q0 + m * M::kOperand + in, 16, 1024), operand(k + in, 16, 1024), sh, x > 0);
+                    }
+                    mma_commit(&S.s_full[buf]);
+                };
+                auto outputs = [&](int m, int buf, int i, bool add) {
+                    const uint32_t v = kv0 + stage * 2 * M::kOperand + M::kOperand;
+                    const int steps = (valid_of(i) + 15) / 16;
+                    constexpr uint32_t sh = shape<DT == DSSD_BF16>(128, DP, true);
+                    for (int x = 0; x < steps; ++x)
+                        mma_ts(tmem + 256 + m * 128, tmem + buf * 128 + x * 8, operand(v + x * 2048, M::kChunk, 1024), sh, add || x > 0);
+                    mma_commit(&S.o_done[m]);
+                };
+                auto step_next = [&]() {
+                    mma_commit(&S.k_empty[next]);
+                    if (++next == M::kStages) next = 0, ++next_round;
+                };
+                const int first = at.tile, last = at.tile + n - 1;
+                if (!(ok = bar_wait(&S.k_full[next], next_round & 1, failed))) break;
+                tc_after();
+                for (int m = 0; m < kMT; ++m) scores(m, kMT == 1 ? sbuf : m, first);
+                if (kMT == 1) sbuf ^= 1;
+                step_next();
+                for (int i = first; i <= last && ok; ++i) {
+                    if (kMT == 1 && i < last) {
+                        if (!(ok = bar_wait(&S.k_full[next], next_round & 1, failed))) break;
+                        tc_after();
+                        scores(0, sbuf, i + 1);
+                        sbuf ^= 1;
+                        step_next();
+                    }
+                    for (int m = 0; m < kMT; ++m) {
+                        // (one tile of rows: P of tile i is in the buffer that tile i + 1 did not take)
+                        const int buf = kMT == 1 ? (i < last ? sbuf : sbuf ^ 1) : m;
+                        if (!(ok = bar_wait(&S.p_ready[buf], p_phase[buf], failed))) break;
+                        p_phase[buf] ^= 1;
+                        if (m == 0 && !(ok = bar_wait(&S.v_full[stage], round & 1, failed))) break;
+                        if (i == first && items && !(ok = bar_wait(&S.o_free[m], (items - 1) & 1, failed))) break;
+                        tc_after();
+                        outputs(m, buf, i, i > first);
+                        if (m == kMT - 1) mma_commit(&S.v_empty[stage]);
+                        if (kMT == 2 && i < last) {
+                            if (m == 0 && !(ok = bar_wait(&S.k_full[next], next_round & 1, failed))) break;
+                            tc_after();
+                            scores(m, m, i + 1);
+                            if (m == kMT - 1) step_next();
+                        }
+                    }
+                    if (++stage == M::kStages) stage = 0, ++round;
+                }
+                if (ok) mma_commit(&S.q_empty);
+                ++items;
+                left -= n;
+                advance(P, at);
+            }
+            // the last arrival that the tensor core owes this CTA's shared memory
+            if (ok && items) bar_wait(&S.q_empty, (items - 1) & 1, failed);
         }
-        if (threadIdx.x < (unsigned)P.D)
-            static_cast<unsigned short *>(P.o)[b * P.o_b + j * P.o_n + hq * P.o_h + threadIdx.x] = bits<DT>(ot / lt);
-        if (threadIdx.x == 0 && P.lse) P.lse[(b * P.N + j) * P.Hq + hq] = mt + logf(lt);
+        __syncwarp();
+    } else if (warp >= 4) {
+        // ---- softmax: a thread per row
+        const int m = (warp - 4) / 4;
+        const int row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        int stage = 0;
+        unsigned round = 0, s_phase[2] = {0, 0}, o_count = 0;
+        bool ok = true;
+        int sbuf = kMT == 1 ? 0 : m;
+        const long long range_start = left;  // (a segment that begins here is the piece's first)
+        const int node_in = row / P.G;
+        const int head_in = row - node_in * P.G;
+        const float inf = __int_as_float(0x7f800000);
+        while (left > 0 && ok) {
+            const int h = at.item / P.row_items, rt = at.item - h * P.row_items;
+            const int n = (int)(left < at.tiles - at.tile ? left : at.tiles - at.tile);
+            const int node = (rt * kMT + m) * P.nodes_per_tile + node_in;
+            const bool in_tile = node_in < P.nodes_per_tile && node < P.N;
+            bool there = in_tile;
+            float top = DSSD_NEG_INF, sum = 0.f;  // the maximum that weights refer to, in units of S
+            uint32_t sees[4] = {0, 0, 0, 0};      // the row's node's ancestors and itself
+            bool no_key = false;                  // there is no node `row`
+            if (at.tile == 0) {
+                short *const parent = S.parent[warp - 4];
+                bool bad = false;
+                __syncwarp();
+                for (int j = lane; j < P.N; j += 32) {
+                    int p = j - 1;
+                    if (j > 0 && P.parents) p = ld_after(P.parents + at.b * (P.N - 1) + j - 1);
+                    bad |= j > 0 && p >= j;
+                    parent[j] = (short)(j == 0 ? 0 : p >= j ? -1 : max(p, -1));
+                }
+                __syncwarp();
+                if (in_tile) {
+                    int up = node;
+                    while (up > 0) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (up >> 5 == k) sees[k] |= 1u << (up & 31);
+                        up = parent[up];
+                    }
+                    there = up == 0;  // else there is no way to the root, and no node here
+                    sees[0] |= 1u;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (!there) sees[k] = 0;
+                }
+                if (row < P.N) {
+                    int up = row;
+                    while (up > 0) up = parent[up];
+                    no_key = up < 0;
+                    bad |= no_key && parent[row] >= 0;
+                }
+                if (bad && h == 0 && rt == 0 && m == 0 && P.flags) atomicOr(P.flags + at.b, DSSD_CACHE_FLAG_BAD_NODE);
+            }
+            for (int i = at.tile; i < at.tile + n; ++i) {
+                if (!(ok = warp_wait(&S.s_full[sbuf], s_phase[sbuf], failed))) break;
+                s_phase[sbuf] ^= 1;
+                tc_after();
+                const int valid = i == 0 ? P.N : min(kTile, at.ctx - (i - 1) * kTile);
+                const int parts = (valid + 31) / 32;
+                const uint32_t sp = tmem + sbuf * 128 + lanes;
+                // which of 32 columns count
+                auto allowed = [&](int part) {
+                    const uint32_t s = part == 0 ? sees[0] : part == 1 ? sees[1] : part == 2 ? sees[2] : sees[3];
+                    const int v = valid - part * 32;
+                    return (i == 0 ? s : 0xffffffffu) & (v >= 32 ? 0xffffffffu : (1u << v) - 1u);
+                };
+                const bool masked = i == 0 || valid < kTile;
+                float hi = DSSD_NEG_INF;
+                for (int part = 0; part < parts; ++part) {
+                    uint32_t s[32];
+                    tmem_ld32(sp + part * 32, s);
+                    tmem_ld_wait();
+                    if (masked) {
+                        const uint32_t a = allowed(part);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if ((a >> k) & 1u) hi = fmaxf(hi, __uint_as_float(s[k]));
+                    } else {
+                        float h4[4] = {DSSD_NEG_INF, DSSD_NEG_INF, DSSD_NEG_INF, DSSD_NEG_INF};
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) h4[k & 3] = fmaxf(h4[k & 3], __uint_as_float(s[k]));
+                        hi = fmaxf(hi, fmaxf(fmaxf(h4[0], h4[1]), fmaxf(h4[2], h4[3])));
+                    }
+                }
+                const bool begin = i == at.tile;
+                bool o_known = begin;
+                const bool raise = hi > top && (hi - top) * P.c > 8.f;  // (top = -inf: the first keys that count)
+                if (__any_sync(0xffffffffu, raise)) {
+                    const float f = raise ? (top == DSSD_NEG_INF ? 0.f : ex2((top - hi) * P.c)) : 1.f;
+                    if (raise) top = hi;
+                    sum *= f;
+                    if (!begin) {
+                        if (!(ok = warp_wait(&S.o_done[m], (o_count - 1) & 1, failed))) break;
+                        o_known = true;
+                        tc_after();
+                        for (int x = 0; x < DP; x += 32) {
+                            uint32_t o[32];
+                            tmem_ld32(tmem + 256 + m * 128 + lanes + x, o);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                            tmem_st32(tmem + 256 + m * 128 + lanes + x, o);
+                        }
+                    }
+                }
+                const float ref = top == DSSD_NEG_INF ? 0.f : -top * P.c;
+                const f32x2 c2 = pack2(P.c, P.c), ref2 = pack2(ref, ref);
+                f32x2 part_sum = pack2(0.f, 0.f);
+                for (int part = 0; part < parts; ++part) {
+                    uint32_t s[32], p[16];
+                    tmem_ld32(sp + part * 32, s);
+                    tmem_ld_wait();
+                    if (masked) {
+                        const uint32_t a = allowed(part);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (!((a >> k) & 1u)) s[k] = 0xff800000u;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        float x, y;
+                        unpack2(fma2(pack2(__uint_as_float(s[2 * k]), __uint_as_float(s[2 * k + 1])), c2, ref2), x, y);
+                        x = ex2(x);
+                        y = ex2(y);
+                        part_sum = add2(part_sum, pack2(x, y));
+                        p[k] = pack<DT>(x, y);
+                    }
+                    tmem_st16(sp + part * 16, p);
+                }
+                float even, odd;
+                unpack2(part_sum, even, odd);
+                sum += even + odd;
+                tmem_st_wait();
+                tc_before();
+                if (masked && m == 0) {
+                    // what lies behind the last key, or belongs to no node, is made zero: its weight is, but zero times NaN is not
+                    if (!(ok = warp_wait(&S.v_full[stage], round & 1, failed))) break;
+                    const int upto = (valid + 15) / 16 * 16;
+                    if (row < upto && (row >= valid || (i == 0 && no_key))) {
+                        unsigned char *v = base + M::kKV + stage * 2 * M::kOperand + M::kOperand + row * 128;
+                        for (int x = 0; x < kChunks; ++x)
+                            for (int y = 0; y < 128; y += 16) *reinterpret_cast<uint4 *>(v + x * M::kChunk + y) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_async();
+                }
+                // The tile before has to be in O before this one's weights are given away: a barrier tells its last two phases
+                // apart and no more.  (It is, as a rule.)
+                if (!o_known && !(ok = warp_wait(&S.o_done[m], (o_count - 1) & 1, failed))) break;
+                bar_arrive(&S.p_ready[sbuf]);
+                ++o_count;
+                if (kMT == 1) sbuf ^= 1;
+                if (++stage == M::kStages) stage = 0, ++round;
+            }
+            if (!ok) {
+                if (P.flags) atomicOr(P.flags + at.b, DSSD_CACHE_FLAG_TIMEOUT);
+                break;
+            }
+            if (!(ok = warp_wait(&S.o_done[m], (o_count - 1) & 1, failed))) break;
+            tc_after();
+            const bool whole = n == at.tiles;
+            if (whole) {
+                const float inv = 1.f / sum;
+                const int head = h * P.G + head_in;
+                unsigned short *to = static_cast<unsigned short *>(P.o) + at.b * P.o_b + node * P.o_n + head * P.o_h;
+                for (int x = 0; x < DP; x += 32) {
+                    uint32_t o[32];
+                    __syncwarp();
+                    tmem_ld32(tmem + 256 + m * 128 + lanes + x, o);
+                    tmem_ld_wait();
+                    if (!there) continue;
+#pragma unroll
+                    for (int k = 0; k < 32; k += 8) {
+                        if (x + k >= P.D) break;
+                        uint4 w;
+                        w.x = pack<DT>(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv);
+                        w.y = pack<DT>(__uint_as_float(o[k + 2]) * inv, __uint_as_float(o[k + 3]) * inv);
+                        w.z = pack<DT>(__uint_as_float(o[k + 4]) * inv, __uint_as_float(o[k + 5]) * inv);
+                        w.w = pack<DT>(__uint_as_float(o[k + 6]) * inv, __uint_as_float(o[k + 7]) * inv);
+                        *reinterpret_cast<uint4 *>(to + x + k) = w;
+                    }
+                }
+                if (there && P.lse) P.lse[(at.b * P.N + node) * (P.Hkv * P.G) + head] = top * P.scale + logf(sum);
+            } else {
+                const long long slot = 2ll * blockIdx.x + (left == range_start ? 0 : 1);
+                const long long r = slot * (kMT * 128) + m * 128 + row;
+                float *to = P.part + r * DP;
+                for (int x = 0; x < DP; x += 32) {
+                    uint32_t o[32];
+                    __syncwarp();
+                    tmem_ld32(tmem + 256 + m * 128 + lanes + x, o);
+                    tmem_ld_wait();
+                    if (!in_tile) continue;
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4) *reinterpret_cast<uint4 *>(to + x + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                }
+                // a row without a node is marked by the piece that has tile 0
+                if (in_tile) P.part_ml[r] = make_float2(there ? top * P.c : inf, sum);
+            }
+            tc_before();
+            bar_arrive(&S.o_free[m]);
+            left -= n;
+            advance(P, at);
+        }
     }
-    if (flags && P.flags && lane == 0) atomicOr(P.flags + b, flags);
+    __syncwarp();
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (S.failed) {  // copies in flight are waited for, with a limit, before the shared memory goes
+        if (t == 0)
+            for (int i = 0; i < M::kStages; ++i)
+                for (unsigned k = 0; k < 1u << 16 && !(bar_try(&S.k_full[i], 0) && bar_try(&S.v_full[i], 0)) && !(bar_try(&S.k_full[i], 1) && bar_try(&S.v_full[i], 1)); ++k)
+                    ;
+        __syncthreads();
+    }
+    if (warp == 2) tmem_free(tmem, 512);
+}
+
+// Joins the pieces of items that lie in several: a warp per row.
+template <int DT, int DP, int kMT>
+__global__ void __launch_bounds__(kThreads) tree_join_kernel(const __grid_constant__ Geometry P)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int rows = P.nodes_per_tile * P.G;  // of a tile
+    const unsigned groups = (unsigned)((kMT * rows + kWarps - 1) / kWarps);
+    const unsigned group = blockIdx.x % groups, rest = blockIdx.x / groups;
+    const unsigned items = (unsigned)(P.Hkv * P.row_items);
+    const unsigned item = rest % items;
+    const long long b = rest / items;
+    const int h = item / P.row_items, rt = item - h * P.row_items;
+    const int x = (int)(group * kWarps) + warp;
+    const int m = x / rows, row = x - m * rows;
+    const int node = (rt * kMT + m) * P.nodes_per_tile + row / P.G;
+    pdl_wait();
+    pdl_trigger();
+    if (m >= kMT || node >= P.N) return;
+    const Line line = measure(P, b, false);
+    const long long tiles = tiles_of(length(P, b));
+    const long long n = pieces(line.total, (unsigned)min((long long)kMaxCtas, line.total));
+    const long long x0 = line.before + item * tiles, x1 = x0 + tiles - 1;
+    const long long c0 = ((x0 + 1) * n - 1) / line.total, c1 = ((x1 + 1) * n - 1) / line.total;
+    if (c0 == c1) return;
+    auto slot_row = [&](long long c) {
+        const bool first = c > c0 || c * line.total / n == x0;
+        return (2 * c + (first ? 0 : 1)) * (kMT * 128) + m * 128 + row;
+    };
+    const float2 head = P.part_ml[slot_row(c0)];
+    if (head.x == __int_as_float(0x7f800000)) return;
+    float top = DSSD_NEG_INF;
+    for (long long c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, P.part_ml[slot_row(c)].x);
+    top = warp_max(top);
+    float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    const bool mine = lane * 4 < DP;
+#pragma unroll 4
+    for (long long c = c0; c <= c1; ++c) {
+        const long long r = slot_row(c);
+        const float2 ml = P.part_ml[r];
+        const float w = ex2(ml.x - top);
+        sum += w * ml.y;
+        if (mine) {
+            const float4 v = *reinterpret_cast<const float4 *>(P.part + r * DP + lane * 4);
+            o[0] += w * v.x, o[1] += w * v.y, o[2] += w * v.z, o[3] += w * v.w;
+        }
+    }
+    const float inv = 1.f / sum;
+    const int hq = h * P.G + row % P.G;
+    if (lane * 4 < P.D) {
+        unsigned short *to = static_cast<unsigned short *>(P.o) + b * P.o_b + node * P.o_n + hq * P.o_h + lane * 4;
+        *reinterpret_cast<uint2 *>(to) = make_uint2(pack<DT>(o[0] * inv, o[1] * inv), pack<DT>(o[2] * inv, o[3] * inv));
+    }
+    // lse = ln 2 * log2 of the sum over all weights
+    if (lane == 0 && P.lse) P.lse[(b * P.N + node) * (P.Hkv * P.G) + hq] = top * 0.693147180559945309f + logf(sum);
+}
+
+typedef CUresult (*Encode)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
+                           CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// A map of 16-bit values: sizes from the innermost dimension on, strides (in elements) of the others, the box that a copy takes
+template <int kDims>
+bool encode(CUtensorMap *map, int dtype, const void *at, const int64_t (&size)[kDims], const int64_t (&stride)[kDims - 1], const int (&box)[kDims])
+{
+    static const Encode fn = driver_call<Encode>("cuTensorMapEncodeTiled");
+    if (!fn) return false;
+    cuuint64_t sizes[kDims], strides[kDims - 1];
+    cuuint32_t boxes[kDims], ones[kDims];
+    for (int i = 0; i < kDims; ++i) {
+        sizes[i] = (cuuint64_t)size[i];
+        boxes[i] = (cuuint32_t)box[i];
+        ones[i] = 1;
+        // (the stride of a dimension of one entry is never used, but has to be a stride)
+        if (i) strides[i - 1] = size[i] > 1 ? (cuuint64_t)stride[i - 1] * 2 : 16;
+    }
+    return fn(map, dtype == DSSD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, kDims, const_cast<void *>(at), sizes, strides, boxes, ones,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DT, int DP, int kMT>
+cudaError_t launch_as(const Geometry &P, unsigned grid, unsigned join_grid, cudaStream_t stream)
+{
+    typedef Smem<DP, kMT> M;
+    static PerContext allowed;
+    const int ok = allowed.get([] { return (int)(cudaFuncSetAttribute(tree_attention_kernel<DT, DP, kMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)M::kBytes) == cudaSuccess); });
+    if (!ok) {
+        const cudaError_t e = cudaGetLastError();
+        return e == cudaSuccess ? cudaErrorInvalidConfiguration : e;
+    }
+    const cudaError_t e = launch_pdl(tree_attention_kernel<DT, DP, kMT>, grid, kThreadsOf[kMT], stream, P, M::kBytes);
+    return e == cudaSuccess ? launch_pdl(tree_join_kernel<DT, DP, kMT>, join_grid, kThreads, stream, P) : e;
+}
+
+// values of a piece's row in the workspace, rows of a piece
+int padded(int D) { return D <= 64 ? 64 : 128; }
+int rows_of(int N, int Hq, int Hkv)
+{
+    const int per = 128 / (Hq / Hkv);
+    return N <= per ? 128 : 256;
 }
 
 }  // namespace
 
 size_t tree_attention_workspace(int B, int N, int Hq, int Hkv, int D)
 {
-    (void)B, (void)N, (void)Hq, (void)Hkv, (void)D;
-    return 256;
+    (void)B, (void)Hkv;
+    // (no less for fewer key heads: rows by the query heads, of which each key head has a part)
+    const size_t rows = (long long)N * Hq <= 64 ? 128 : 256;
+    return 2 * (size_t)kMaxCtas * rows * ((size_t)padded(D) * 4 + 8);
 }
 
 cudaError_t tree_attention_launch(TreeAttentionParams &P, int dtype, void *workspace, cudaStream_t stream)
 {
-    (void)workspace;
-    const unsigned grid = (unsigned)P.B * (unsigned)P.N * (unsigned)P.Hq;
-    return dtype == DSSD_BF16 ? launch_pdl(plain_attention_kernel<DSSD_BF16>, grid, kAT, stream, P)
-                              : launch_pdl(plain_attention_kernel<DSSD_F16>, grid, kAT, stream, P);
+    Geometry g;
+    const int G = P.Hq / P.Hkv, per = 128 / G;
+    const int rows = rows_of(P.N, P.Hq, P.Hkv), mt = rows / 128;
+    int box = P.page_size, r = 128;
+    while (r) {
+        const int k = box % r;
+        box = r;
+        r = k;
+    }
+    const bool none = P.num_pages == 0;
+    const int64_t pages = none ? 1 : P.num_pages, page = none ? 1 : P.page_size;
+    const void *kc = none ? P.k_new : P.k_cache, *vc = none ? P.v_new : P.v_cache;
+    bool ok = encode<5>(&g.q, dtype, P.q, {P.D, G, P.Hkv, P.N, P.B}, {P.q_h, G * P.q_h, P.q_n, P.q_b}, {64, G, 1, per, 1});
+    ok = ok && encode<4>(&g.k_new, dtype, P.k_new, {P.D, P.Hkv, P.N, P.B}, {P.new_h, P.new_n, P.new_b}, {64, 1, P.N, 1});
+    ok = ok && encode<4>(&g.v_new, dtype, P.v_new, {P.D, P.Hkv, P.N, P.B}, {P.new_h, P.new_n, P.new_b}, {64, 1, P.N, 1});
+    ok = ok && encode<4>(&g.k_cache, dtype, kc, {P.D, none ? 1 : P.Hkv, page, pages}, {P.cache_h, P.cache_t, P.cache_p}, {64, 1, box, 1});
+    ok = ok && encode<4>(&g.v_cache, dtype, vc, {P.D, none ? 1 : P.Hkv, page, pages}, {P.cache_h, P.cache_t, P.cache_p}, {64, 1, box, 1});
+    if (!ok) return cudaErrorInvalidValue;
+    g.block_table = P.block_table;
+    g.table_stride = P.table_stride;
+    g.max_pages = P.max_pages, g.num_pages = P.num_pages, g.page_size = P.page_size, g.box = box;
+    g.ctx_len = P.ctx_len, g.parents = P.parents;
+    g.B = P.B, g.N = P.N, g.Hkv = P.Hkv, g.G = G, g.D = P.D;
+    g.nodes_per_tile = per;
+    g.row_items = (P.N + mt * per - 1) / (mt * per);
+    g.scale = P.scale;
+    g.c = P.scale * 1.4426950408889634074f;
+    g.o = P.o;
+    g.o_b = P.o_b, g.o_n = P.o_n, g.o_h = P.o_h;
+    g.lse = P.lse;
+    g.flags = P.flags;
+    const int dp = padded(P.D);
+    g.part = static_cast<float *>(workspace);
+    g.part_ml = reinterpret_cast<float2 *>(g.part + 2 * (size_t)kMaxCtas * rows * dp);
+    const long long items = (long long)P.B * P.Hkv * g.row_items;
+    const unsigned join = (unsigned)(items * ((mt * per * G + kWarps - 1) / kWarps));
+    const bool bf = dtype == DSSD_BF16;
+    if (dp == 64) {
+        if (mt == 1) return bf ? launch_as<DSSD_BF16, 64, 1>(g, kMaxCtas, join, stream) : launch_as<DSSD_F16, 64, 1>(g, kMaxCtas, join, stream);
+        return bf ? launch_as<DSSD_BF16, 64, 2>(g, kMaxCtas, join, stream) : launch_as<DSSD_F16, 64, 2>(g, kMaxCtas, join, stream);
+    }
+    if (mt == 1) return bf ? launch_as<DSSD_BF16, 128, 1>(g, kMaxCtas, join, stream) : launch_as<DSSD_F16, 128, 1>(g, kMaxCtas, join, stream);
+    return bf ? launch_as<DSSD_BF16, 128, 2>(g, kMaxCtas, join, stream) : launch_as<DSSD_F16, 128, 2>(g, kMaxCtas, join, stream);
 }
 
 }  // namespace dssd
