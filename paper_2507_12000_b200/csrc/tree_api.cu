@@ -61,8 +61,9 @@ dssd_status dssd_adjust_logits(const void *logits, dssd_dtype dtype, int64_t row
     if (mask_row && !mask && mask_rows > 0) return DSSD_ERR_INVALID_ARG;
     if (mask && !mask_row && (long long)mask_rows < (long long)B * N) return DSSD_ERR_INVALID_ARG;
     if (K > 65535 || L >= 1 << 29) return DSSD_ERR_UNSUPPORTED;
-    // one CTA per slice of 1024 entries at the most
-    if ((long long)B * ((V + 1023) / 1024) > 0x7fffffff) return DSSD_ERR_UNSUPPORTED;
+    // CTAs of the copy
+    const long long per = dssd::adjust_copy_entries((int)dtype);
+    if ((long long)B * N * ((V + per + 7) / per) > 0x7fffffff) return DSSD_ERR_UNSUPPORTED;
 
     dssd::AdjustParams P{};
     P.logits = logits;

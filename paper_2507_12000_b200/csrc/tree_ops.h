@@ -23,10 +23,13 @@ struct AdjustParams {
     uint32_t *flags;
     int B, N, V, L, K, mask_rows;
     // geometry
-    int slices;        // CTAs per sequence, a slice of the vocabulary each
-    int slice;         // entries of a slice, a multiple of 1024
-    int segments;      // pieces of 1024 entries that a row's slice touches
+    int pieces;  // of a row, each a turn of a CTA of the copy
+    int turns;   // CTAs of the copy per row
+    int slots;   // of the patch's table, a power of two
+    int shares;  // CTAs of the patch per sequence
+    int after_copy;
 };
+int adjust_copy_entries(int dtype);  // of a row, by a CTA of the copy
 cudaError_t adjust_launch(AdjustParams &P, int dtype, cudaStream_t stream);
 
 struct TreeVerifyParams {

@@ -62,6 +62,7 @@ def check(got, d, ref, mag, live, before, what=""):
     (2, 128, 33, torch.bfloat16, 9, 40, 4, True), (4, 5, 1000, torch.bfloat16, 300, 7, 0, False), (3, 7, 1025, torch.float32, 77, 0, 5, True),
     (2, 6, 4095, torch.bfloat16, 2100, 300, 6, True), (1, 9, 50272, torch.float32, 600, 32, 2, False), (5, 3, 9001, torch.bfloat16, 5000, 9, 1, True),
     (1, 2, 151936, torch.bfloat16, 100, 3, 1, True), (300, 2, 515, torch.float32, 5, 2, 3, True), (160, 3, 4104, torch.bfloat16, 20, 4, 9, True),
+    (2, 3, 40000, torch.float32, 13000, 9, 2, True), (3, 2, 17000, torch.bfloat16, 20000, 2000, 0, False),
     (3, 4, 777, torch.float32, 0, 0, 4, True), (2, 3, 2048, torch.bfloat16, 0, 5, 0, False),
 ])
 @pytest.mark.parametrize("in_place", [False, True])
