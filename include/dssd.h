@@ -702,7 +702,7 @@ size_t dssd_tree_verify_workspace_bytes(int B, int N, int V);
  * For a chain this is dssd_dsd_verify.
  *
  * Only the rows of nodes on the accepted path are read, and draft rows of those with a rejection.
- * p, sums and the draw are evaluated in float64 (exponentials to about 1e-13).  u == 1 never accepts; q <= 0 accepts iff the left over p > 0; a
+ * p, sums and the draw are evaluated in float64 (exponentials to 5e-11).  T is at most 1e30.  u == 1 never accepts; q <= 0 accepts iff the left over p > 0; a
  * NaN q or an out-of-range token rejects.
  *
  * target_logits [B, N, V] float32 or bfloat16, row (b, j) at element (b*N+j)*row_stride

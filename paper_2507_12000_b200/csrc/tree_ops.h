@@ -43,6 +43,7 @@ struct TreeVerifyParams {
     int32_t *accept_len, *path, *token;
     uint32_t *edge_flags, *rs_flags;
     int slice;  // entries of the vocabulary per CTA of the sequence's cluster
+    int chunk;  // entries of a warp at a time
 };
 size_t tree_verify_workspace(int B, int N, int V);
 cudaError_t tree_verify_launch(TreeVerifyParams &P, int dtype, void *workspace, cudaStream_t stream);

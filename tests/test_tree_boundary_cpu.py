@@ -71,7 +71,7 @@ def verify(B, /, **kw):
 @pytest.mark.parametrize("kw,status", [
     (dict(logits=None), 1), (dict(draft_q=None), 1), (dict(draft_tokens=None), 1), (dict(uniforms=None), 1), (dict(uniforms_rs=None), 1),
     (dict(accept_len=None), 1), (dict(path=None), 1), (dict(token=None), 1), (dict(T=0.0), 1), (dict(T=float("inf")), 1), (dict(row_stride=99), 1),
-    (dict(B=0), 1), (dict(N=0), 1), (dict(V=0), 1), (dict(logits=P + 2), 1), (dict(draft_q=P + 1), 1), (dict(dtype=2), 2), (dict(N=129), 2),
+    (dict(B=0), 1), (dict(N=0), 1), (dict(V=0), 1), (dict(logits=P + 2), 1), (dict(draft_q=P + 1), 1), (dict(dtype=2), 2), (dict(N=129), 2), (dict(T=2e30), 2),
     (dict(workspace=None), 3), (dict(workspace=P + 8), 3), (dict(bytes=0), 3),
 ])
 def test_verify_refuses(B, kw, status):

@@ -113,6 +113,16 @@ def test_rows_out_of_order(B):
         same(call(B, d, 1.0, False), R.verify(d, 1.0, False))
 
 
+@pytest.mark.parametrize("T,shift", [(0.001, 0.0), (0.01, 3.0e4), (1.0, -3.0e4), (1e20, 0.0)])
+def test_sums_beyond_the_range_of_float64(B, T, shift):
+    """Scaled logits of thousands: the row is summed relative to its maximum.  At T = 1e20 only masked entries differ from the others."""
+    rng = np.random.default_rng(12)
+    d = R.verify_inputs(rng, 5, 4, 2000, torch.float32, window=2, ragged=False)
+    d["target_logits"] += shift
+    d["target_logits"][:, :, ::3] = float("-inf")
+    same(call(B, d, T, True), R.verify(d, T, True))
+
+
 def test_p_equal_to_q_falls_back(B):
     """A rejection by u = 1 where p = q leaves no mass: the token comes from p."""
     x = torch.zeros(2, 2, 64, device="cuda")
