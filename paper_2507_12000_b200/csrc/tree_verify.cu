@@ -11,12 +11,12 @@
 // and one exchange, a rejection one pass over both rows and one exchange; the last of these passes leaves the sums of chunks that the draw
 // picks from.  A warp takes a chunk of 512 entries at a time.
 //
-// The draw compares a uniform with sums over 10^5 terms: an error of 1e-7 in p, in the sum or in a would move a step of the distribution past the
-// uniform once in a few hundred draws.  So p and the sums are float64: 2^x by a table of 16 entries (each in banks of its own: no conflicts) and a
-// polynomial.  No maximum is needed, since float64 holds 2^(+-1000): a row whose sum leaves that range is taken again, relative to its maximum.
+// The tests and the draw are decisions: what is wanted is the answer that exact arithmetic gives.  A pass in float32 (3 to 5 instructions an entry)
+// gives p, its sums and m with known bounds on their errors, and a comparison further apart than those is certain.
+// One that is not, as a rule a draw whose uniform falls within 10^-6 of a step of the distribution, takes the node again in float64 (25 to 35 instructions an
+// entry: 2^x by a table of 16 entries, each in banks of its own, and a polynomial).  With everything in float64 the verdicts of B=128 N=12 V=151936 took 232 us.
 //
-// Bound by the latency of a chain of dependent reductions for few sequences; by the float64 pipes (10 to 12 operations an entry) and the visited
-// rows for many.
+// Bound by the latency of a chain of dependent reductions for few sequences, by the visited rows for many.
 #include "launch.h"
 #include "quads.cuh"
 #include "tree.cuh"
@@ -32,14 +32,21 @@ constexpr int kBlock = 512;       // entries that a warp loads at once
 
 struct VerifySmem {
     double table[16];
-    double part[2][kMaxCluster][2];  // what the CTAs of the cluster exchange, in turns
-    double warp[kWarps][2];
+    double part[2][kMaxCluster];  // what the CTAs of the cluster exchange, in turns
+    double warp[2][kWarps];
     double chunk[kMaxChunks];
-    double own, picked;
+    double own;
     int token[kMaxNodes];
     short parent[kMaxNodes], child[kMaxNodes], sibling[kMaxNodes];
-    int bad, found;
+    int bad;
+    unsigned long long again[1];  // the draw was not certain
 };
+
+// Bounds of the errors of a float32 pass, relative to the whole distribution: a sum of p over any entries, divided by the row's.  Per term:
+// ex2 2^-22; the rounding of x = l c1 - ref, 2^-25 |x|, of which p weighs 17 bits at the most for 10^5 entries; sixteen float32 additions in a tree of
+// four.  Twice that, for the row's sum.  (c1 is rounded to float32 on this path: p is that of a temperature 3e-8 off, 1e-7 of p.)
+constexpr double kSumError = 1.5e-6;
+constexpr double kProductError = 2.5e-7;  // of a q in the residual, for each unit of a
 
 __device__ __forceinline__ double as_double(int hi, int lo) { return __hiloint2double(hi, lo); }
 
@@ -71,36 +78,25 @@ __device__ __forceinline__ double exp2_64(double x, const double *table)
     return as_double(yh, far ? 0 : __double2loint(y));
 }
 
-struct Two {
-    double a, b;
-};
-
-// (a, b) of all threads, warps in order and CTAs in rank order; the same in every thread.  own: this CTA's a.
-__device__ Two cluster_sum(VerifySmem &S, Two v, unsigned ctas, int &turn)
+// x of all threads, warps in order and CTAs in rank order; the same in every thread
+__device__ __forceinline__ double cluster_sum(VerifySmem &S, double x, unsigned ctas, int &turn)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    v.a = warp_sum(v.a);
-    v.b = warp_sum(v.b);
-    if (lane == 0) S.warp[warp][0] = v.a, S.warp[warp][1] = v.b;
+    x = warp_sum(x);
+    if (lane == 0) S.warp[turn][warp] = x;
     __syncthreads();
-    Two s = {0.0, 0.0};
+    double s = 0.0;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) s.a += S.warp[w][0], s.b += S.warp[w][1];
-    if (ctas == 1) {
-        __syncthreads();
-        return s;
+    for (int w = 0; w < kWarps; ++w) s += S.warp[turn][w];
+    if (ctas > 1) {
+        if (threadIdx.x < ctas) cluster_store(&S.part[turn][cluster_rank()], threadIdx.x, s);
+        cluster_arrive();
+        cluster_wait();
+        s = 0.0;
+        for (unsigned c = 0; c < ctas; ++c) s += S.part[turn][c];
     }
-    const unsigned me = cluster_rank();
-    if (threadIdx.x < ctas) {
-        cluster_store(&S.part[turn][me][0], threadIdx.x, s.a);
-        cluster_store(&S.part[turn][me][1], threadIdx.x, s.b);
-    }
-    cluster_arrive();
-    cluster_wait();
-    Two all = {0.0, 0.0};
-    for (unsigned c = 0; c < ctas; ++c) all.a += S.part[turn][c][0], all.b += S.part[turn][c][1];
-    turn ^= 1;
-    return all;
+    turn ^= 1;  // (a thread that is here again has seen every other thread's arrival at the exchange between)
+    return s;
 }
 
 template <int DT>
@@ -111,6 +107,12 @@ struct Logits<DSSD_BF16> {
     static constexpr uint32_t kFill = 0xff80u;
     __device__ static uint32_t bits(const uint2 &v, int i) { return i == 0 ? v.x << 16 : i == 1 ? v.x & 0xffff0000u : i == 2 ? v.y << 16 : v.y & 0xffff0000u; }
     __device__ static uint32_t one(const char *row, int v) { return ld_row_u16(row + 2ll * v) << 16; }
+    __device__ static float max16(const uint2 (&w)[4])
+    {
+        uint32_t m = max_bf16x2(max_bf16x2(w[0].x, w[0].y), max_bf16x2(w[1].x, w[1].y));
+        m = max_bf16x2(m, max_bf16x2(max_bf16x2(w[2].x, w[2].y), max_bf16x2(w[3].x, w[3].y)));
+        return fmaxf(bf16_lo(m), bf16_hi(m));
+    }
 };
 template <>
 struct Logits<DSSD_F32> {
@@ -118,12 +120,43 @@ struct Logits<DSSD_F32> {
     static constexpr uint32_t kFill = 0xff800000u;
     __device__ static uint32_t bits(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
     __device__ static uint32_t one(const char *row, int v) { return ld_row_u32(row + 4ll * v); }
+    __device__ static float max16(const uint4 (&w)[4])
+    {
+        float m = DSSD_NEG_INF;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(w[u].x), __uint_as_float(w[u].y)), fmaxf(__uint_as_float(w[u].z), __uint_as_float(w[u].w))));
+        return m;
+    }
 };
 __device__ __forceinline__ bool is_nan(uint32_t w) { return (w & 0x7fffffffu) > 0x7f800000u; }
 
+// A CTA's slice of a row, by chunks of whole blocks
+struct Slice {
+    int V, v0, v1, chunk, chunks;
+};
+
+// A warp's blocks: those of its chunks, one after the other
+struct Walk {
+    const Slice &P;
+    int k, at;
+    __device__ __forceinline__ Walk(const Slice &p, int warp) : P(p), k(warp), at(p.v0 + warp * p.chunk) {}
+    __device__ __forceinline__ bool more() const { return k < P.chunks; }
+    __device__ __forceinline__ bool next()  // whether the chunk ends with the block that is left
+    {
+        at += kBlock;
+        if (at < min(P.v1, P.v0 + (k + 1) * P.chunk)) return false;
+        k += kWarps;
+        at = P.v0 + k * P.chunk;
+        return true;
+    }
+};
+
+__device__ __forceinline__ int exponent(double x) { return ((__double2hiint(x) >> 20) & 0x7ff) - 1023; }
+
 // kShift: rows may begin off the boundaries of four entries
 template <int DT, bool kShift>
-__global__ void __launch_bounds__(kThreads, 3) tree_verify_kernel(const __grid_constant__ TreeVerifyParams P)
+__global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_constant__ TreeVerifyParams P)
 {
     typedef Logits<DT> E;
     __shared__ VerifySmem S;
@@ -134,6 +167,7 @@ __global__ void __launch_bounds__(kThreads, 3) tree_verify_kernel(const __grid_c
     const long long b = blockIdx.x / ctas;
     const int v0 = (int)min((long long)P.V, (long long)me * P.slice), v1 = (int)min((long long)P.V, (long long)v0 + P.slice);
     const int chunks = (v1 - v0 + P.chunk - 1) / P.chunk;
+    const Slice slice = {P.V, v0, v1, P.chunk, chunks};
     if (t < 16) S.table[t] = exp2(t / 16.0);
     pdl_wait();
     pdl_trigger();
@@ -158,7 +192,9 @@ __global__ void __launch_bounds__(kThreads, 3) tree_verify_kernel(const __grid_c
 
     int node = 0, length = 0;
     double a = 0.0, m = 1.0, c = 1.0, gone = 0.0, ref = 0.0, sum = 1.0, inv = 1.0;
-    bool alive = true;
+    double a_error = 0.0, m_error = 0.0;
+    bool alive = true, fine = false;
+    const float c1 = (float)P.c1;
     const char *row;
     const float *qrow;
     // what a test needs, asked for before the pass that comes before it
@@ -178,223 +214,368 @@ __global__ void __launch_bounds__(kThreads, 3) tree_verify_kernel(const __grid_c
         }
         return r;
     };
-    auto lse_pass = [&](bool keep) {
-        Two s = {0.0, 0.0};
-        for (int k = warp; k < chunks; k += kWarps) {
-            double part = 0.0;
-            unsigned odd = 0;
-            for (int at = v0 + k * P.chunk; at < min(v1, v0 + (k + 1) * P.chunk); at += kBlock) {
-                WarpQuads<typename E::Q, 4, kShift> L;
-                L.load(row, P.V, at, E::kFill);
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const typename E::Q::Raw w = L.at(u);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t x = E::bits(w, i);
-                        odd |= is_nan(x);
-                        part += exp2_64(__fma_rn(widen<DT>(x), P.c1, -ref), S.table);
-                    }
-                }
-            }
-            s.b += odd ? 1.0 : 0.0;
-            if (keep) {
-                part = warp_sum(part);
-                if (lane == 0) S.chunk[k] = part;
-                s.a += lane == 0 ? part : 0.0;
-            } else
-                s.a += part;
-        }
-        return s;
-    };
-    auto rest_pass = [&](bool keep) {  // in units of the row's sum
-        double total = 0.0;
-        const double aS = a * sum;
-        for (int k = warp; k < chunks; k += kWarps) {
-            double part = 0.0;
-            for (int at = v0 + k * P.chunk; at < min(v1, v0 + (k + 1) * P.chunk); at += kBlock) {
-                WarpQuads<typename E::Q, 4, kShift> L;
-                WarpQuads<Quads32, 4, kShift> R;
-                L.load(row, P.V, at, E::kFill);
-                R.load(reinterpret_cast<const char *>(qrow), P.V, at, 0u);
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const typename E::Q::Raw w = L.at(u);
-                    const uint4 q = R.at(u);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const double e = exp2_64(__fma_rn(widen<DT>(E::bits(w, i)), P.c1, -ref), S.table);
-                        const uint32_t qb = i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w;
-                        const double r = __fma_rn(-aS, widen<DSSD_F32>(qb), e);  // (a q of zero is 2^-127: below any p)
-                        part += r > 0.0 ? r : 0.0;
-                    }
-                }
-            }
-            if (keep) {
-                part = warp_sum(part);
-                if (lane == 0) S.chunk[k] = part;
-                total += lane == 0 ? part : 0.0;
-            } else
-                total += part;
-        }
-        return total;
+    // the sum of a chunk, where the draw will want it
+    auto close = [&](bool keep, bool ends, int k, double &part, double &total) {
+        if (!keep || !ends) return;
+        part = warp_sum(part);
+        if (lane == 0) S.chunk[k] = part, total += part;
+        part = 0.0;
     };
     if (me == 0 && t == 0) P.path[b * P.N] = 0;
-    bool has_child, kept;
+    bool relative = false, plain = false;  // take the row relative to its maximum (in ref); draw from p after all
     while (true) {
         row = static_cast<const char *>(P.logits) + (b * P.N + node) * P.row_stride * (long long)E::Q::kBytes;
         qrow = P.draft_q + (b * P.N + node) * (long long)P.V;
-        int j = S.child[node];
-        has_child = j > 0;
-        kept = !has_child;  // the pass leaves the chunks' sums
+        int j = plain ? 0 : S.child[node];
+        const bool has_child = S.child[node] > 0;
+        bool kept = j == 0;  // the pass leaves the chunks' sums
+        bool certain = true;
         Asked next = ask(j);
-        ref = 0.0;
-        Two all = cluster_sum(S, lse_pass(kept), ctas, turn);
-        alive = all.b == 0.0;
-        if (alive && !(all.a > 1e-280 && all.a < 1e280)) {
-            // out of range: relative to the row's maximum, which the CTAs find by the same exchange, each for itself
-            float mx = DSSD_NEG_INF;
-            for (int v = t; v < P.V; v += kThreads) mx = fmaxf(mx, __uint_as_float(E::one(row, v)));
-            mx = warp_max(mx);
-            __syncthreads();
-            if (lane == 0) S.warp[warp][0] = (double)mx;
-            __syncthreads();
-            double top = S.warp[0][0];
-            for (int w = 1; w < kWarps; ++w) top = fmax(top, S.warp[w][0]);
-            __syncthreads();
-            alive = top > -1e300 && top < 1e300;
-            if (alive) {
-                ref = top * P.c1;
-                all = cluster_sum(S, lse_pass(kept), ctas, turn);
+        if (!relative) ref = 0.0;
+        {
+            // the sum of 2^(l c1 - ref); NaN where the row holds one, or +inf
+            double part = 0.0, total = 0.0;
+            Walk w(slice, warp);
+            if (!fine) {
+                WarpQuads<typename E::Q, 4, kShift> N;
+                if (w.more()) N.load(row, P.V, w.at, E::kFill);
+                while (w.more()) {
+                    typename E::Q::Raw q[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) q[u] = N.at(u);
+                    const int k = w.k;
+                    const bool ends = w.next();
+                    if (w.more()) N.load(row, P.V, w.at, E::kFill);  // on its way while this block is summed
+                    // relative to a whole power of two near the lane's largest term, so that its sum's scaling is exact
+                    float r = ceilf(E::max16(q) * c1);
+                    r = r > -1000.f ? r : -1000.f;
+                    f32x2 acc[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+                    const f32x2 c2 = pack2(c1, c1), r2 = pack2(-r, -r);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            float x, y;
+                            unpack2(fma2(pack2(__uint_as_float(E::bits(q[u], 2 * i)), __uint_as_float(E::bits(q[u], 2 * i + 1))), c2, r2), x, y);
+                            acc[i] = add2(acc[i], pack2(ex2(x), ex2(y)));
+                        }
+                    float x, y;
+                    unpack2(add2(acc[0], acc[1]), x, y);
+                    part += (double)(x + y) * as_double((1023 + (int)fminf(r, 1000.f)) << 20, 0);
+                    close(kept, ends, k, part, total);
+                }
+            } else {
+                while (w.more()) {
+#pragma unroll 1
+                    for (int half = 0; half < kBlock; half += kBlock / 2) {
+                        WarpQuads<typename E::Q, 2, kShift> L;
+                        L.load(row, P.V, w.at + half, E::kFill);
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const typename E::Q::Raw q = L.at(u);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t x = E::bits(q, i);
+                                part += exp2_64(__fma_rn(widen<DT>(x), P.c1, -ref), S.table);
+                                if (is_nan(x)) part = __longlong_as_double(0x7ff8000000000000ll);
+                            }
+                        }
+                    }
+                    const int k = w.k;
+                    close(kept, w.next(), k, part, total);
+                }
+            }
+            sum = cluster_sum(S, kept ? total : part, ctas, turn);
+        }
+        alive = sum == sum;
+        if (alive && !(sum > 1e-280 && sum < 1e280)) {
+            if (!fine) {
+                fine = true;
+                continue;
+            }
+            // out of range: relative to the row's maximum, which each CTA finds for itself
+            alive = false;
+            if (!relative) {
+                float mx = DSSD_NEG_INF;
+                for (int v = t; v < P.V; v += kThreads) mx = fmaxf(mx, __uint_as_float(E::one(row, v)));
+                mx = warp_max(mx);
+                __syncthreads();
+                if (lane == 0) S.warp[0][warp] = (double)mx;
+                __syncthreads();
+                double top = S.warp[0][0];
+                for (int w = 1; w < kWarps; ++w) top = fmax(top, S.warp[0][w]);
+                __syncthreads();
+                if (top > -1e300 && top < 1e300) {
+                    ref = top * P.c1;
+                    relative = true;
+                    continue;
+                }
             }
         }
         if (!alive) eflags |= DSSD_EDGE_FLAG_NONFINITE;
-        sum = all.a;
         inv = 1.0 / sum;
         a = 0.0, m = 1.0, c = 1.0, gone = 0.0;
+        a_error = m_error = 0.0;
+        const double slack = fine ? 0.0 : kSumError, C = fine ? P.c1 : (double)c1;
         bool taken = false;
         while (j > 0) {
             if (!next.ok) eflags |= DSSD_EDGE_FLAG_BAD_TOKEN;
-            const double qx = (double)next.q, u = (double)next.u;
-            const double px = exp2_64(__fma_rn(widen<DT>(next.l), P.c1, -ref), S.table) * inv;
-            const double left = fmax(px - a * qx, 0.0);
-            if (next.ok && alive && u < 1.0 && (qx <= 0.0 ? left > 0.0 : u * (c * m) * qx < left)) {
-                taken = true;
-                break;
+            if (next.ok && alive) {
+                const double qx = (double)next.q, u = (double)next.u;
+                const double px = exp2_64(__fma_rn(widen<DT>(next.l), C, -ref), S.table) * inv;
+                const double left = fmax(px - a * qx, 0.0), want = u * (c * m) * qx;
+                taken = u < 1.0 && (qx <= 0.0 ? left > 0.0 : want < left);
+                // (a NaN q rejects, whatever the errors)
+                if (!fine && u < 1.0 && qx > 0.0 && !(fabs(px - a * qx - want) > px * slack + qx * (a_error + u * c * m_error))) {
+                    certain = false;
+                    break;
+                }
+                if (taken) break;
             }
             // rejected: what is left of p
             a += c * m;
+            a_error += c * m_error;
             if (!P.replacement) {
-                if (next.ok && qx > 0.0) gone += qx;
+                if (next.ok && next.q > 0.f) gone += (double)next.q;
                 c = 1.0 / fmax(1.0 - gone, 1e-300);  // (nothing left of q: p where q has no mass)
+            }
+            if (!fine && alive && !(a < 1e6)) {
+                certain = false;
+                break;
             }
             j = S.sibling[j];
             next = ask(j);
             kept = j == 0;
-            m = alive ? cluster_sum(S, {rest_pass(kept), 0.0}, ctas, turn).a * inv : 0.0;
-        }
-        if (!taken) break;
-        node = j;
-        ++length;
-        if (me == 0 && t == 0) P.path[b * P.N + length] = j;
-    }
-
-    // the draw, from p or from max(0, p - a q), both in units of the row's sum
-    if (!has_child) rflags |= DSSD_RS_FLAG_BONUS;
-    if (a > 0.0 && !(m > 0.0)) {
-        rflags |= DSSD_RS_FLAG_FALLBACK;
-        a = 0.0;
-        if (alive) cluster_sum(S, lse_pass(true), ctas, turn);
-    }
-    const double aS = a * sum;
-    auto mass = [&](int v) {
-        double r = exp2_64(__fma_rn(widen<DT>(E::one(row, v)), P.c1, -ref), S.table);
-        if (a > 0.0) r = __fma_rn(-aS, widen<DSSD_F32>(ld_row_u32(qrow + v)), r);
-        return r > 0.0 ? r : 0.0;
-    };
-    __syncthreads();
-    // a CTA's sum is that of its chunks in order
-    if (warp == 0) {
-        double s = 0.0;
-        for (int k = lane; k < chunks; k += 32) s += alive ? S.chunk[k] : 0.0;
-        s = warp_sum(s);
-        if (lane == 0) S.own = s;
-    }
-    __syncthreads();
-    const double own = S.own;
-    if (ctas > 1) {
-        if (t < (int)ctas) cluster_store(&S.part[turn][me][0], t, own);
-        cluster_arrive();
-        cluster_wait();
-    }
-    double total = 0.0;
-    for (unsigned k = 0; k < ctas; ++k) total += ctas > 1 ? S.part[turn][k][0] : own;
-    const double target = (double)ld_after(P.uniforms_rs + b) * total;
-    int owner = -1, last = 0;  // last: the last CTA with mass
-    double run = 0.0, before = 0.0;
-    for (unsigned k = 0; k < ctas; ++k) {
-        const double w = ctas > 1 ? S.part[turn][k][0] : own;
-        if (w > 0.0) last = (int)k;
-        if (owner < 0 && run + w > target) owner = (int)k, before = run;
-        run += w;
-    }
-    const bool invalid = !alive || !(total > 0.0);
-    const bool short_of = owner < 0;  // rounding left none: the last entry with mass
-    if (short_of) owner = last;
-    if (invalid) rflags |= DSSD_RS_FLAG_INVALID;
-    if (me == (unsigned)(invalid ? 0 : owner) && warp == 0) {
-        int token = -1;
-        if (!invalid) {
-            // the chunk, 32 at a time
-            double r = before;
-            int pick = -1, lastk = 0;
-            for (int k0 = 0; k0 < chunks && pick < 0; k0 += 32) {
-                const int k = k0 + lane;
-                const double w = k < chunks ? S.chunk[k] : 0.0;
-                double cum = w;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const double up = __shfl_up_sync(0xffffffffu, cum, o);
-                    if (lane >= o) cum += up;
+            m = 0.0;
+            if (!alive) continue;
+            // the sum of max(0, p - a q): in float64 in units of the row's sum, in float32 in units of the power of two below it
+            double part = 0.0, total = 0.0;
+            Walk w(slice, warp);
+            if (!fine) {
+                const int e = exponent(sum);
+                const float aF = (float)(a * sum * as_double((1023 - e) << 20, 0));
+                const f32x2 c2 = pack2(c1, c1), r2 = pack2(-(float)e, -(float)e), a2 = pack2(-aF, -aF);
+                WarpQuads<typename E::Q, 4, kShift> N;
+                WarpQuads<Quads32, 4, kShift> NQ;
+                if (w.more()) {
+                    N.load(row, P.V, w.at, E::kFill);
+                    NQ.load(reinterpret_cast<const char *>(qrow), P.V, w.at, 0u);
                 }
-                const unsigned some = __ballot_sync(0xffffffffu, w > 0.0);
-                if (some) lastk = k0 + 31 - __clz(some);
-                const unsigned over = __ballot_sync(0xffffffffu, !short_of && w > 0.0 && r + cum > target);
-                if (over) {
-                    const int l = __ffs(over) - 1;
-                    pick = k0 + l;
-                    const double upto = __shfl_sync(0xffffffffu, cum, l), its = __shfl_sync(0xffffffffu, w, l);
-                    r += upto - its;
-                } else
-                    r += __shfl_sync(0xffffffffu, cum, 31);
+                while (w.more()) {
+                    typename E::Q::Raw l[4];
+                    uint4 q[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) l[u] = N.at(u), q[u] = NQ.at(u);
+                    const int k = w.k;
+                    const bool ends = w.next();
+                    if (w.more()) {
+                        N.load(row, P.V, w.at, E::kFill);
+                        NQ.load(reinterpret_cast<const char *>(qrow), P.V, w.at, 0u);
+                    }
+                    f32x2 acc[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+                    float x, y;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            unpack2(fma2(pack2(__uint_as_float(E::bits(l[u], 2 * i)), __uint_as_float(E::bits(l[u], 2 * i + 1))), c2, r2), x, y);
+                            const f32x2 q2 = i == 0 ? pack2(__uint_as_float(q[u].x), __uint_as_float(q[u].y)) : pack2(__uint_as_float(q[u].z), __uint_as_float(q[u].w));
+                            unpack2(fma2(a2, q2, pack2(ex2(x), ex2(y))), x, y);
+                            acc[i] = add2(acc[i], pack2(fmaxf(x, 0.f), fmaxf(y, 0.f)));
+                        }
+                    unpack2(add2(acc[0], acc[1]), x, y);
+                    part += (double)(x + y);
+                    close(kept, ends, k, part, total);
+                }
+                m = (kept ? total : part) * as_double((1023 + e) << 20, 0);
+            } else {
+                const double aS = a * sum;
+                while (w.more()) {
+#pragma unroll 1
+                    for (int half = 0; half < kBlock; half += kBlock / 2) {
+                        WarpQuads<typename E::Q, 2, kShift> L;
+                        WarpQuads<Quads32, 2, kShift> R;
+                        L.load(row, P.V, w.at + half, E::kFill);
+                        R.load(reinterpret_cast<const char *>(qrow), P.V, w.at + half, 0u);
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const typename E::Q::Raw l = L.at(u);
+                            const uint4 q = R.at(u);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const double p = exp2_64(__fma_rn(widen<DT>(E::bits(l, i)), P.c1, -ref), S.table);
+                                const uint32_t qb = i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w;
+                                const double d = __fma_rn(-aS, widen<DSSD_F32>(qb), p);  // (a q of zero is 2^-127: below any p)
+                                part += d > 0.0 ? d : 0.0;
+                            }
+                        }
+                    }
+                    const int k = w.k;
+                    close(kept, w.next(), k, part, total);
+                }
+                m = kept ? total : part;
             }
-            const bool hit = pick >= 0;
-            const int k = hit ? pick : lastk;
-            int last_v = -1;
-            const int e = min(v1, v0 + (k + 1) * P.chunk);
-            for (int base = v0 + k * P.chunk; base < e && token < 0; base += 128) {
-                // four runs of 32 entries: their loads together
-                double w[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = base + 32 * i + lane < e ? mass(base + 32 * i + lane) : 0.0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    double cum = w[i];
+            m = cluster_sum(S, m, ctas, turn) * inv;
+            m_error = slack + a_error + (1.0 + a) * (fine ? 0.0 : kProductError);
+            if (!fine && !(m > 8.0 * m_error)) {  // what is left is no more than the errors
+                certain = false;
+                break;
+            }
+        }
+        if (!certain) {
+            fine = true;
+            continue;
+        }
+        if (taken) {
+            node = j;
+            ++length;
+            fine = relative = false;
+            if (me == 0 && t == 0) P.path[b * P.N + length] = j;
+            continue;
+        }
+
+        // the draw, from p or from max(0, p - a q)
+        rflags = has_child ? (plain ? DSSD_RS_FLAG_FALLBACK : 0u) : DSSD_RS_FLAG_BONUS;
+        if (a > 0.0 && !(m > 0.0)) {
+            if (alive) {  // the row's own sums once more
+                plain = true;
+                continue;
+            }
+            rflags |= DSSD_RS_FLAG_FALLBACK;
+        }
+        // entries in units of the chunks' sums
+        const bool scaled = !fine && a > 0.0;
+        const double unit = scaled ? as_double((1023 - exponent(sum)) << 20, 0) : 1.0;
+        const double aS = a * sum;
+        auto mass = [&](int v) {
+            double r = exp2_64(__fma_rn(widen<DT>(E::one(row, v)), C, -ref), S.table);
+            if (a > 0.0) r = __fma_rn(-aS, widen<DSSD_F32>(ld_row_u32(qrow + v)), r);
+            return r > 0.0 ? r * unit : 0.0;
+        };
+        __syncthreads();
+        // a CTA's sum is that of its chunks in order
+        if (warp == 0) {
+            double s = 0.0;
+            for (int k = lane; k < chunks; k += 32) s += alive ? S.chunk[k] : 0.0;
+            s = warp_sum(s);
+            if (lane == 0) S.own = s;
+        }
+        __syncthreads();
+        const double own = S.own;
+        if (ctas > 1) {
+            if (t < (int)ctas) cluster_store(&S.part[turn][me], t, own);
+            cluster_arrive();
+            cluster_wait();
+        }
+        double total = 0.0;
+        for (unsigned k = 0; k < ctas; ++k) total += ctas > 1 ? S.part[turn][k] : own;
+        const double target = (double)ld_after(P.uniforms_rs + b) * total;
+        int owner = -1, last = 0;  // last: the last CTA with mass
+        double run = 0.0, before = 0.0;
+        for (unsigned k = 0; k < ctas; ++k) {
+            const double w = ctas > 1 ? S.part[turn][k] : own;
+            if (w > 0.0) last = (int)k;
+            if (owner < 0 && run + w > target) owner = (int)k, before = run;
+            run += w;
+        }
+        turn ^= 1;
+        const bool invalid = !alive || !(total > 0.0);
+        const bool short_of = owner < 0;  // rounding left none: the last entry with mass
+        if (short_of) owner = last;
+        if (invalid) rflags |= DSSD_RS_FLAG_INVALID;
+        if (invalid) owner = 0;
+        // the uniform's place and the steps of the distribution have to be further apart than this
+        const double margin = fine ? -1.0 : 2.0 * sum * unit * (a > 0.0 ? m_error : kSumError);
+        if (me == (unsigned)owner && warp == 0) {
+            int token = -1;
+            bool sure = true;
+            if (!invalid) {
+                // the chunk, 32 at a time
+                double r = before;
+                int pick = -1, lastk = 0;
+                for (int k0 = 0; k0 < chunks && pick < 0; k0 += 32) {
+                    const int k = k0 + lane;
+                    const double w = k < chunks ? S.chunk[k] : 0.0;
+                    double cum = w;
 #pragma unroll
                     for (int o = 1; o < 32; o <<= 1) {
                         const double up = __shfl_up_sync(0xffffffffu, cum, o);
                         if (lane >= o) cum += up;
                     }
-                    const unsigned some = __ballot_sync(0xffffffffu, w[i] > 0.0);
-                    if (some) last_v = base + 32 * i + 31 - __clz(some);
-                    const unsigned over = __ballot_sync(0xffffffffu, w[i] > 0.0 && r + cum > target);
-                    if (hit && over && token < 0) token = base + 32 * i + __ffs(over) - 1;
+                    const unsigned some = __ballot_sync(0xffffffffu, w > 0.0);
+                    if (some) lastk = k0 + 31 - __clz(some);
+                    const unsigned over = __ballot_sync(0xffffffffu, !short_of && w > 0.0 && r + cum > target);
+                    if (over) {
+                        const int l = __ffs(over) - 1;
+                        pick = k0 + l;
+                        const double upto = __shfl_sync(0xffffffffu, cum, l), its = __shfl_sync(0xffffffffu, w, l);
+                        r += upto - its;
+                    } else
+                        r += __shfl_sync(0xffffffffu, cum, 31);
+                }
+                const bool hit = pick >= 0;
+                const int k = hit ? pick : lastk;
+                int last_v = -1;
+                sure = fine;
+                const int e = min(v1, v0 + (k + 1) * P.chunk);
+                for (int base = v0 + k * P.chunk; base < e && token < 0; base += kBlock) {
+                    // sixteen neighbouring entries to a lane, all loads together
+                    const int v = base + lane * 16;
+                    double w[16], mine = 0.0;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) w[i] = v + i < e ? mass(v + i) : 0.0;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) mine += w[i];
+                    double cum = mine;
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const double up = __shfl_up_sync(0xffffffffu, cum, o);
+                        if (lane >= o) cum += up;
+                    }
+                    const unsigned some = __ballot_sync(0xffffffffu, mine > 0.0);
+                    const unsigned over = __ballot_sync(0xffffffffu, hit && mine > 0.0 && r + cum > target);
+                    // the lane that the target is in, or the last with mass
+                    const int l = over ? __ffs(over) - 1 : some ? 31 - __clz(some) : -1;
+                    if (l >= 0) {
+                        double run2 = r + cum - mine;
+                        int found = -1, lastw = -1;
+                        bool fits = false;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            if (w[i] > 0.0) lastw = v + i;
+                            if (found < 0 && w[i] > 0.0 && run2 + w[i] > target) {
+                                found = v + i;
+                                fits = target - run2 > margin && run2 + w[i] - target > margin;
+                            }
+                            run2 += w[i];
+                        }
+                        const int f = __shfl_sync(0xffffffffu, found, l), lw = __shfl_sync(0xffffffffu, lastw, l);
+                        const bool ft = __shfl_sync(0xffffffffu, (int)fits, l) != 0;
+                        last_v = lw;
+                        if (over) {
+                            token = f >= 0 ? f : lw;  // (the lane's sum and its entries' differ by their rounding)
+                            sure = sure || (f >= 0 && ft);
+                        }
+                    }
                     r += __shfl_sync(0xffffffffu, cum, 31);
                 }
+                if (token < 0) token = last_v;
             }
-            if (token < 0) token = last_v;
+            if (lane == 0 && sure) P.token[b] = token;
+            if (ctas > 1) {
+                if (lane < (int)ctas) cluster_store(&S.again[0], lane, (unsigned long long)!sure);
+            } else if (lane == 0)
+                S.again[0] = !sure;
         }
-        if (lane == 0) P.token[b] = token;
+        // (a CTA's shared memory outlives the others' stores into it)
+        if (ctas > 1) {
+            cluster_arrive();
+            cluster_wait();
+        } else
+            __syncthreads();
+        if (!S.again[0]) break;
+        fine = true;
+        __syncthreads();
     }
     if (me == 0) {
         for (int k = length + 1 + t; k < P.N; k += kThreads) P.path[b * P.N + k] = -1;
@@ -403,10 +584,6 @@ __global__ void __launch_bounds__(kThreads, 3) tree_verify_kernel(const __grid_c
             if (P.edge_flags) P.edge_flags[b] = eflags;
             if (P.rs_flags) P.rs_flags[b] = rflags;
         }
-    }
-    if (ctas > 1) {  // (a CTA's shared memory outlives the others' stores into it)
-        cluster_arrive();
-        cluster_wait();
     }
 }
 
