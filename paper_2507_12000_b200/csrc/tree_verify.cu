@@ -35,7 +35,6 @@ struct VerifySmem {
     double part[2][kMaxCluster];  // what the CTAs of the cluster exchange, in turns
     double warp[2][kWarps];
     double chunk[kMaxChunks];
-    double own;
     int token[kMaxNodes];
     short parent[kMaxNodes], child[kMaxNodes], sibling[kMaxNodes];
     int bad;
@@ -152,6 +151,13 @@ struct Walk {
     }
 };
 
+// whole 16-byte pieces of `bytes` at p
+__device__ __forceinline__ void prefetch_l2(const void *p, int bytes)
+{
+    const uintptr_t from = (reinterpret_cast<uintptr_t>(p) + 15) & ~(uintptr_t)15, to = (reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes) & ~(uintptr_t)15;
+    if (to > from) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"((uint32_t)(to - from)) : "memory");
+}
+
 __device__ __forceinline__ int exponent(double x) { return ((__double2hiint(x) >> 20) & 0x7ff) - 1023; }
 
 // kShift: rows may begin off the boundaries of four entries
@@ -187,6 +193,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
         cluster_wait();
     }
     __syncthreads();
+    const double u_draw = (double)ld_after(P.uniforms_rs + b);
     int turn = 0;
     unsigned eflags = S.bad ? DSSD_EDGE_FLAG_BAD_PARENT : 0u, rflags = 0;
 
@@ -232,6 +239,11 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
         bool certain = true;
         Asked next = ask(j);
         if (!relative) ref = 0.0;
+        if (j > 0 && t == 0 && v1 > v0) {
+            // What comes next is asked of memory now: this CTA's part of q, which a rejection reads, and of the first child's row.
+            prefetch_l2(qrow + v0, (v1 - v0) * 4);
+            prefetch_l2(static_cast<const char *>(P.logits) + ((b * P.N + j) * P.row_stride + v0) * (long long)E::Q::kBytes, (v1 - v0) * E::Q::kBytes);
+        }
         {
             // the sum of 2^(l c1 - ref); NaN where the row holds one, or +inf
             double part = 0.0, total = 0.0;
@@ -443,49 +455,27 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
             }
             rflags |= DSSD_RS_FLAG_FALLBACK;
         }
-        // entries in units of the chunks' sums
-        const bool scaled = !fine && a > 0.0;
-        const double unit = scaled ? as_double((1023 - exponent(sum)) << 20, 0) : 1.0;
-        const double aS = a * sum;
-        auto mass = [&](int v) {
-            double r = exp2_64(__fma_rn(widen<DT>(E::one(row, v)), C, -ref), S.table);
-            if (a > 0.0) r = __fma_rn(-aS, widen<DSSD_F32>(ld_row_u32(qrow + v)), r);
-            return r > 0.0 ? r * unit : 0.0;
-        };
-        __syncthreads();
-        // a CTA's sum is that of its chunks in order
-        if (warp == 0) {
-            double s = 0.0;
-            for (int k = lane; k < chunks; k += 32) s += alive ? S.chunk[k] : 0.0;
-            s = warp_sum(s);
-            if (lane == 0) S.own = s;
-        }
-        __syncthreads();
-        const double own = S.own;
-        if (ctas > 1) {
-            if (t < (int)ctas) cluster_store(&S.part[turn][me], t, own);
-            cluster_arrive();
-            cluster_wait();
-        }
-        double total = 0.0;
-        for (unsigned k = 0; k < ctas; ++k) total += ctas > 1 ? S.part[turn][k] : own;
-        const double target = (double)ld_after(P.uniforms_rs + b) * total;
+        // What the exchange after the last pass left: the CTAs' sums, in units of the row's.  The chunks' sums of a float32 pass over p - a q are
+        // in units of a power of two below that.
+        const double unit = !fine && a > 0.0 ? as_double((1023 + exponent(sum)) << 20, 0) : 1.0;
+        const double aS = a * sum, total = a > 0.0 ? m * sum : sum, target = u_draw * total;
+        const double *const parts = S.part[turn ^ 1];
         int owner = -1, last = 0;  // last: the last CTA with mass
         double run = 0.0, before = 0.0;
         for (unsigned k = 0; k < ctas; ++k) {
-            const double w = ctas > 1 ? S.part[turn][k] : own;
+            const double w = ctas > 1 ? parts[k] : total;
             if (w > 0.0) last = (int)k;
             if (owner < 0 && run + w > target) owner = (int)k, before = run;
             run += w;
         }
-        turn ^= 1;
+        __syncthreads();  // (the chunks' sums)
         const bool invalid = !alive || !(total > 0.0);
         const bool short_of = owner < 0;  // rounding left none: the last entry with mass
         if (short_of) owner = last;
         if (invalid) rflags |= DSSD_RS_FLAG_INVALID;
         if (invalid) owner = 0;
         // the uniform's place and the steps of the distribution have to be further apart than this
-        const double margin = fine ? -1.0 : 2.0 * sum * unit * (a > 0.0 ? m_error : kSumError);
+        const double margin = fine ? -1.0 : 2.0 * sum * (a > 0.0 ? m_error : kSumError);
         if (me == (unsigned)owner && warp == 0) {
             int token = -1;
             bool sure = true;
@@ -495,7 +485,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
                 int pick = -1, lastk = 0;
                 for (int k0 = 0; k0 < chunks && pick < 0; k0 += 32) {
                     const int k = k0 + lane;
-                    const double w = k < chunks ? S.chunk[k] : 0.0;
+                    const double w = k < chunks ? S.chunk[k] * unit : 0.0;
                     double cum = w;
 #pragma unroll
                     for (int o = 1; o < 32; o <<= 1) {
@@ -521,9 +511,18 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
                 for (int base = v0 + k * P.chunk; base < e && token < 0; base += kBlock) {
                     // sixteen neighbouring entries to a lane, all loads together
                     const int v = base + lane * 16;
+                    uint32_t l16[16], q16[16];
                     double w[16], mine = 0.0;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) w[i] = v + i < e ? mass(v + i) : 0.0;
+                    for (int i = 0; i < 16; ++i) l16[i] = v + i < e ? E::one(row, v + i) : 0xff800000u;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) q16[i] = a > 0.0 && v + i < e ? ld_row_u32(qrow + v + i) : 0u;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const double p = exp2_64(__fma_rn(widen<DT>(l16[i]), C, -ref), S.table);
+                        const double d = a > 0.0 ? __fma_rn(-aS, widen<DSSD_F32>(q16[i]), p) : p;
+                        w[i] = d > 0.0 ? d : 0.0;
+                    }
 #pragma unroll
                     for (int i = 0; i < 16; ++i) mine += w[i];
                     double cum = mine;
