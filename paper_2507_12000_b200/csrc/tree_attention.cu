@@ -6,6 +6,10 @@
 // its nodes (tile 0, masked by ancestors) and then the cache, 128 positions to a tile, brought in by tiled copies, one per page or part of a
 // page, into a ring of stages; the copies fill what lies outside a head's size with zeros, so any size works on 64 or 128 columns.
 //
+// Two groups of four warps do the softmax, each with an S and an O of its own (tensor memory holds two of each): while one is at its exponentials
+// the tensor core works for the other.  With more than 128 rows each group has a tile of rows; with fewer both have the same rows and every
+// other tile of keys, and the two results are joined at the end.  One group for all keys took 2700 cycles a tile, as long as the cache's bytes take to arrive.
+//
 // What bounds it: the cache's bytes as long as a tile's 64 KB take longer to arrive (2900 cycles of an SM's share of the measured
 // bandwidth) than 128 rows of softmax (128 exponentials a thread, 1024 cycles of the special-function units) and
 // two products (1024 cycles); for 256 rows the products and exponentials come to the same 2048 cycles.
@@ -31,13 +35,15 @@ namespace {
 constexpr int kTile = 128;      // keys of a tile, rows of a tile
 constexpr int kMaxCtas = 148;   // pieces of the line
 constexpr int kMinTiles = 2;    // tiles to a piece at least
-constexpr int kThreadsOf[3] = {0, 256, 384};
+constexpr int kAttend = 384;     // threads: copies, products and two idle warps; the two groups of the softmax
 
 struct Geometry {
     CUtensorMap q, k_new, v_new, k_cache, v_cache;
     const int32_t *block_table;
     int64_t table_stride;
-    int max_pages, num_pages, page_size, box;  // box: positions of a copy, the greatest common divisor of the page and 128
+    int max_pages, num_pages, page_size;
+    int box_log;                // positions of a copy, the greatest common divisor of the page and 128: a power of two
+    int tile_pages, tile_rest;  // 128 divided by the page: the quotient and the rest
     const int32_t *ctx_len, *parents;
     int B, N, Hkv, G, D;
     int nodes_per_tile, row_items;  // nodes in a tile of rows; items of kMT tiles to a key head
@@ -46,8 +52,9 @@ struct Geometry {
     int64_t o_b, o_n, o_h;
     float *lse;
     uint32_t *flags;
-    float *part;     // [2 kMaxCtas][kMT * 128][kDP]
-    float2 *part_ml; // [2 kMaxCtas][kMT * 128] maximum in powers of two, sum
+    float *part;      // [2 kMaxCtas][kMT * 128][kDP]
+    float2 *part_ml;  // [2 kMaxCtas][kMT * 128] maximum in powers of two, sum
+    int4 *joins;      // [kMaxCtas] the item that this piece is the second of: sequence, item, slot of its first piece, its last piece; sequence -1: none
 };
 
 __device__ __forceinline__ int length(const Geometry &P, long long b, bool *bad = nullptr)
@@ -59,28 +66,18 @@ __device__ __forceinline__ int length(const Geometry &P, long long b, bool *bad 
 }
 __device__ __forceinline__ int tiles_of(int ctx) { return 1 + (ctx + kTile - 1) / kTile; }
 
-// all tiles of the line, and of the sequences before b, by one warp (all lanes get both)
-struct Line {
-    long long total, before;
-};
-__device__ Line measure(const Geometry &P, long long b, bool report)
+// all tiles of the line, by one warp (all lanes get it)
+__device__ long long measure(const Geometry &P, bool report)
 {
-    const int lane = threadIdx.x & 31;
-    long long all = 0, before = 0;
-    for (long long i = lane; i < P.B; i += 32) {
+    long long all = 0;
+    for (long long i = threadIdx.x & 31; i < P.B; i += 32) {
         bool bad;
-        const int t = tiles_of(length(P, i, &bad));
+        all += tiles_of(length(P, i, &bad));
         if (report && bad && P.flags) atomicOr(P.flags + i, DSSD_CACHE_FLAG_BAD_LENGTH);
-        all += t;
-        if (i < b) before += t;
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        all += __shfl_xor_sync(0xffffffffu, all, o);
-        before += __shfl_xor_sync(0xffffffffu, before, o);
-    }
-    const long long items = (long long)P.Hkv * P.row_items;
-    return {all * items, before * items};
+    for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+    return all * P.Hkv * P.row_items;
 }
 __device__ __forceinline__ long long pieces(long long total, unsigned grid)
 {
@@ -151,14 +148,15 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi)
 
 template <int DP, int kMT>
 struct Smem {
-    static constexpr int kStages = DP == 64 ? (kMT == 1 ? 6 : 5) : (kMT == 1 ? 3 : 2);
+    static constexpr int kStages = DP == 64 ? (kMT == 1 ? 5 : 5) : (kMT == 1 ? 3 : 2);
     static constexpr int kChunk = kTile * 128;             // 64 columns of a tile
     static constexpr int kOperand = kTile * DP * 2;
     static constexpr int kQ = 0, kKV = kMT * kOperand;     // then K and V of the stages in turn
     static constexpr int kRest = kKV + kStages * 2 * kOperand;
     struct Rest {
-        uint64_t q_full, q_empty, k_full[kStages], v_full[kStages], k_empty[kStages], v_empty[kStages], s_full[2], p_ready[2], o_done[kMT], o_free[kMT];
-        short parent[4 * kMT][128];  // of the nodes, for each warp of the softmax
+        uint64_t q_full, q_empty, k_full[kStages], v_full[kStages], k_empty[kStages], v_empty[kStages], s_full[2], p_ready[2], o_done[2], o_free[2], half;
+        signed char parent[kMT == 1 ? 4 : 8][128];  // of the nodes, for each warp of the softmax that meets tile 0
+        float2 other[kMT == 1 ? 128 : 1];     // maximum and sum of the second group's half of the keys
         Place place;
         long long count;
         uint32_t tmem;
@@ -169,7 +167,7 @@ struct Smem {
 };
 
 template <int DT, int DP, int kMT>
-__global__ void __launch_bounds__(kThreadsOf[kMT], 1) tree_attention_kernel(const __grid_constant__ Geometry P)
+__global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid_constant__ Geometry P)
 {
     typedef Smem<DP, kMT> M;
     extern __shared__ unsigned char raw[];
@@ -190,11 +188,10 @@ __global__ void __launch_bounds__(kThreadsOf[kMT], 1) tree_attention_kernel(cons
         for (int i = 0; i < 2; ++i) {
             bar_init(&S.s_full[i], 1);
             bar_init(&S.p_ready[i], 128);
-        }
-        for (int i = 0; i < kMT; ++i) {
             bar_init(&S.o_done[i], 1);
             bar_init(&S.o_free[i], 128);
         }
+        bar_init(&S.half, 128);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         S.failed = 0;
     }
@@ -209,13 +206,22 @@ __global__ void __launch_bounds__(kThreadsOf[kMT], 1) tree_attention_kernel(cons
     pdl_wait();
     pdl_trigger();
     if (warp == 3) {  // which piece of the line is this CTA's
-        const long long total = measure(P, 0, blockIdx.x == 0).total;
+        const long long total = measure(P, blockIdx.x == 0), c = blockIdx.x;
         const long long n = pieces(total, gridDim.x);
         long long from = 0, to = 0;
-        if ((long long)blockIdx.x < n) from = blockIdx.x * total / n, to = (blockIdx.x + 1ll) * total / n;
+        if (c < n) from = c * total / n, to = (c + 1) * total / n;
         Place p = {0, 0, 0, 1, 0};
         if (to > from) p = find(P, from);
-        if (lane == 0) S.place = p, S.count = to - from;
+        if (lane == 0) {
+            S.place = p, S.count = to - from;
+            // an item that begins in the piece before and goes on here is joined under this piece's number
+            int4 join = make_int4(-1, 0, 0, 0);
+            if (to > from && p.tile > 0) {
+                const long long x0 = from - p.tile, before = (c - 1) * total / n;
+                if (before <= x0) join = make_int4((int)p.b, p.item, 2 * (int)(c - 1) + (before == x0 ? 0 : 1), (int)(((x0 + p.tiles) * n - 1) / total));
+            }
+            P.joins[c] = join;
+        }
     }
     tc_before();
     __syncthreads();
@@ -227,6 +233,7 @@ __global__ void __launch_bounds__(kThreadsOf[kMT], 1) tree_attention_kernel(cons
 
     if (warp == 0) {
         // ---- copies: every lane brings in boxes of its own
+        constexpr int kAhead = 2;
         int stage = 0;
         unsigned round = 0, items = 0;
         bool ok = true;
@@ -241,28 +248,37 @@ __global__ void __launch_bounds__(kThreadsOf[kMT], 1) tree_attention_kernel(cons
                         copy_5d(base + M::kQ + m * M::kOperand + x * M::kChunk, &P.q, &S.q_full, x * 64, 0, h, (rt * kMT + m) * P.nodes_per_tile, (int)at.b);
             }
             ++items;
+            // A lane's boxes of a tile are lane, lane + 32, ...: box x % 128/box of the tile's positions, 64 columns number x / (128/box).  Where the box
+            // of the first lies in its page is carried along from tile to tile (a division each time took longer than the copies).
+            const int full = kTile >> P.box_log, mask = full - 1, all = full * kChunks;
+            const int first = at.tile > 0 ? (at.tile - 1) * kTile : 0;
+            int page_at[kAhead], off[kAhead];
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) {
+                const int p = first + (((lane + 32 * a) & mask) << P.box_log);
+                page_at[a] = p / P.page_size;
+                off[a] = p - page_at[a] * P.page_size;
+            }
+            const int32_t *table = P.block_table + at.b * P.table_stride;
+            auto number = [&](int p) {
+                int pg = ld_after(table + p);
+                if (pg < 0 || pg >= P.num_pages) {
+                    if (P.flags) atomicOr(P.flags + at.b, DSSD_CACHE_FLAG_BAD_PAGE);
+                    pg = max(P.num_pages, 1);  // outside the cache: zeros come
+                }
+                return pg;
+            };
             for (int i = at.tile; ok && i < at.tile + n; ++i) {
                 unsigned char *k = base + M::kKV + stage * 2 * M::kOperand, *v = k + M::kOperand;
                 const int pos = (i - 1) * kTile;
                 const int valid = i == 0 ? P.N : min(kTile, at.ctx - pos);
-                const int boxes = i == 0 ? 1 : (valid + P.box - 1) / P.box;
-                const uint32_t bytes = (uint32_t)(kChunks * 128 * (i == 0 ? P.N : boxes * P.box));
-                // the pages are looked up before the wait for the stage: two boxes to a lane, for pages of four and more
-                constexpr int kAhead = 2;
-                int page[kAhead], off[kAhead];
-                auto lookup = [&](int x, int &pg, int &of) {
-                    const int p = pos + (x % boxes) * P.box;
-                    of = p % P.page_size;
-                    pg = ld_after(P.block_table + at.b * P.table_stride + p / P.page_size);
-                    if (pg < 0 || pg >= P.num_pages) {
-                        if (P.flags) atomicOr(P.flags + at.b, DSSD_CACHE_FLAG_BAD_PAGE);
-                        pg = max(P.num_pages, 1);  // outside the cache: zeros come
-                    }
-                };
-                if (i > 0)
+                const int boxes = (valid + (1 << P.box_log) - 1) >> P.box_log;  // of the cache's tiles
+                const uint32_t bytes = (uint32_t)(kChunks * 128 * (i == 0 ? P.N : boxes << P.box_log));
+                int page[kAhead];
+                if (i > 0)  // the pages are looked up before the wait for the stage
 #pragma unroll
                     for (int a = 0; a < kAhead; ++a)
-                        if (lane + 32 * a < boxes * kChunks) lookup(lane + 32 * a, page[a], off[a]);
+                        if (lane + 32 * a < all && ((lane + 32 * a) & mask) < boxes) page[a] = number(page_at[a]);
                 ok = warp_wait(&S.k_empty[stage], (round & 1) ^ 1, failed);
                 if (!ok) break;
                 if (lane == 0) bar_expect(&S.k_full[stage], bytes);
@@ -274,13 +290,13 @@ __global__ void __launch_bounds__(kThreadsOf[kMT], 1) tree_attention_kernel(cons
                     }
 #pragma unroll
                     for (int a = 0; a < kAhead; ++a) {
-                        const int x = lane + 32 * a;
-                        if (x < boxes * kChunks) copy_4d(to + (x / boxes) * M::kChunk + (x % boxes) * P.box * 128, cache, bar, (x / boxes) * 64, h, off[a], page[a]);
+                        const int x = lane + 32 * a, y = x & mask;
+                        const int chunk = kChunks == 1 ? 0 : x >= full;
+                        if (x < all && y < boxes) copy_4d(to + chunk * M::kChunk + (y << P.box_log) * 128, cache, bar, chunk * 64, h, off[a], page[a]);
                     }
-                    for (int x = lane + 32 * kAhead; x < boxes * kChunks; x += 32) {
-                        int pg, of;
-                        lookup(x, pg, of);
-                        copy_4d(to + (x / boxes) * M::kChunk + (x % boxes) * P.box * 128, cache, bar, (x / boxes) * 64, h, of, pg);
+                    for (int x = lane + 32 * kAhead; x < all; x += 32) {  // (pages of less than four positions)
+                        const int y = x & mask, chunk = kChunks == 1 ? 0 : x >= full, p = pos + (y << P.box_log);
+                        if (y < boxes) copy_4d(to + chunk * M::kChunk + (y << P.box_log) * 128, cache, bar, chunk * 64, h, p % P.page_size, number(p / P.page_size));
                     }
                 };
                 bring(k, &P.k_new, &P.k_cache, &S.k_full[stage]);
@@ -289,6 +305,13 @@ __global__ void __launch_bounds__(kThreadsOf[kMT], 1) tree_attention_kernel(cons
                 if (lane == 0) bar_expect(&S.v_full[stage], bytes);
                 __syncwarp();
                 bring(v, &P.v_new, &P.v_cache, &S.v_full[stage]);
+                if (i > 0)
+#pragma unroll
+                    for (int a = 0; a < kAhead; ++a) {  // 128 positions on
+                        page_at[a] += P.tile_pages;
+                        off[a] += P.tile_rest;
+                        if (off[a] >= P.page_size) off[a] -= P.page_size, ++page_at[a];
+                    }
                 if (++stage == M::kStages) stage = 0, ++round;
             }
             left -= n;
@@ -299,66 +322,80 @@ __global__ void __launch_bounds__(kThreadsOf[kMT], 1) tree_attention_kernel(cons
         if (lane == 0) {
             int stage = 0, next = 0;  // of PV, of QK
             unsigned round = 0, next_round = 0, items = 0;
-            unsigned p_phase[2] = {0, 0};
+            unsigned p_phase[2] = {0, 0}, uses[2] = {0, 0};
             bool ok = true;
-            const uint32_t q0 = smem_u32(base + M::kQ), kv0 = smem_u32(base + M::kKV);
-            int sbuf = 0;  // (one tile of rows) the buffer of the next S
+            const uint64_t q_operand = operand(smem_u32(base + M::kQ), 16, 1024), k_operand = operand(smem_u32(base + M::kKV), 16, 1024);
+            const uint64_t v_operand = operand(smem_u32(base + M::kKV + M::kOperand), M::kChunk, 1024);
             while (left > 0 && ok) {
                 const int n = (int)(left < at.tiles - at.tile ? left : at.tiles - at.tile);
                 ok = bar_wait(&S.q_full, items & 1, failed);
                 if (!ok) break;
                 auto valid_of = [&](int i) { return i == 0 ? P.N : min(kTile, at.ctx - (i - 1) * kTile); };
-                auto scores = [&](int m, int buf, int i) {
-                    const uint32_t k = kv0 + next * 2 * M::kOperand;
-                    const uint32_t sh = shape<DT == DSSD_BF16>(128, (valid_of(i) + 15) / 16 * 16, false);
+                // Operands step by adding to the low word of their descriptors (a place in shared memory, by 16 bytes; it never carries): made
+                // anew for every product they took longer than the products.
+                // S of group g for the tile of keys i
+                auto scores = [&](int g, int i) {
+                    const uint64_t q = q_operand + (kMT == 2 ? g * (M::kOperand >> 4) : 0), k = k_operand + next * (2 * M::kOperand >> 4);
+                    const int valid = valid_of(i);
+                    const uint32_t sh = valid == kTile ? shape<DT == DSSD_BF16>(128, 128, false) : shape<DT == DSSD_BF16>(128, (valid + 15) / 16 * 16, false);
 #pragma unroll
                     for (int x = 0; x < DP / 16; ++x) {
-                        const uint32_t in = (x / 4) * M::kChunk + (x % 4) * 32;
-                        mma_ss(tmem + buf * 128, operand(q0 + m * M::kOperand + in, 16, 1024), operand(k + in, 16, 1024), sh, x > 0);
+                        const uint32_t in = ((x / 4) * M::kChunk + (x % 4) * 32) >> 4;
+                        mma_ss(tmem + g * 128, q + in, k + in, sh, x > 0);
                     }
-                    mma_commit(&S.s_full[buf]);
+                    mma_commit(&S.s_full[g]);
                 };
-                auto outputs = [&](int m, int buf, int i, bool add) {
-                    const uint32_t v = kv0 + stage * 2 * M::kOperand + M::kOperand;
-                    const int steps = (valid_of(i) + 15) / 16;
+                auto outputs = [&](int g, int i, bool add) {
+                    const uint64_t v = v_operand + stage * (2 * M::kOperand >> 4);
                     constexpr uint32_t sh = shape<DT == DSSD_BF16>(128, DP, true);
-                    for (int x = 0; x < steps; ++x)
-                        mma_ts(tmem + 256 + m * 128, tmem + buf * 128 + x * 8, operand(v + x * 2048, M::kChunk, 1024), sh, add || x > 0);
-                    mma_commit(&S.o_done[m]);
+                    const int steps = (valid_of(i) + 15) / 16;
+                    const uint32_t o = tmem + 256 + g * 128, p = tmem + g * 128;
+#pragma unroll
+                    for (int x = 0; x < 8; ++x)
+                        if (x < steps) mma_ts(o, p + x * 8, v + x * (2048 >> 4), sh, add || x > 0);
+                    mma_commit(&S.o_done[g]);
                 };
                 auto step_next = [&]() {
                     mma_commit(&S.k_empty[next]);
                     if (++next == M::kStages) next = 0, ++next_round;
                 };
+                auto key_tile = [&]() {
+                    const bool there = bar_wait(&S.k_full[next], next_round & 1, failed);
+                    tc_after();
+                    return there;
+                };
                 const int first = at.tile, last = at.tile + n - 1;
-                if (!(ok = bar_wait(&S.k_full[next], next_round & 1, failed))) break;
-                tc_after();
-                for (int m = 0; m < kMT; ++m) scores(m, kMT == 1 ? sbuf : m, first);
-                if (kMT == 1) sbuf ^= 1;
-                step_next();
-                for (int i = first; i <= last && ok; ++i) {
-                    if (kMT == 1 && i < last) {
-                        if (!(ok = bar_wait(&S.k_full[next], next_round & 1, failed))) break;
-                        tc_after();
-                        scores(0, sbuf, i + 1);
-                        sbuf ^= 1;
+                // the S that need no P before them
+                if (kMT == 2) {
+                    if (!(ok = key_tile())) break;
+                    scores(0, first);
+                    scores(1, first);
+                    step_next();
+                } else
+                    for (int g = 0; g < 2 && g < n && ok; ++g) {
+                        if (!(ok = key_tile())) break;
+                        scores(g, first + g);
                         step_next();
                     }
-                    for (int m = 0; m < kMT; ++m) {
-                        // (one tile of rows: P of tile i is in the buffer that tile i + 1 did not take)
-                        const int buf = kMT == 1 ? (i < last ? sbuf : sbuf ^ 1) : m;
-                        if (!(ok = bar_wait(&S.p_ready[buf], p_phase[buf], failed))) break;
-                        p_phase[buf] ^= 1;
-                        if (m == 0 && !(ok = bar_wait(&S.v_full[stage], round & 1, failed))) break;
-                        if (i == first && items && !(ok = bar_wait(&S.o_free[m], (items - 1) & 1, failed))) break;
+                for (int i = first; i <= last && ok; ++i) {
+                    for (int g = kMT == 2 ? 0 : (i - first) & 1; g < 2 && ok; g += kMT == 2 ? 1 : 2) {
+                        const bool begin = i - first < (kMT == 2 ? 1 : 2);  // the group's first tile of this item
+                        if (!(ok = bar_wait(&S.p_ready[g], p_phase[g], failed))) break;
+                        p_phase[g] ^= 1;
+                        if ((kMT == 1 || g == 0) && !(ok = bar_wait(&S.v_full[stage], round & 1, failed))) break;
+                        if (begin) {
+                            if (uses[g] && !(ok = bar_wait(&S.o_free[g], (uses[g] - 1) & 1, failed))) break;
+                            ++uses[g];
+                        }
                         tc_after();
-                        outputs(m, buf, i, i > first);
-                        if (m == kMT - 1) mma_commit(&S.v_empty[stage]);
-                        if (kMT == 2 && i < last) {
-                            if (m == 0 && !(ok = bar_wait(&S.k_full[next], next_round & 1, failed))) break;
-                            tc_after();
-                            scores(m, m, i + 1);
-                            if (m == kMT - 1) step_next();
+                        outputs(g, i, !begin);
+                        if (kMT == 1 || g == 1) mma_commit(&S.v_empty[stage]);
+                        // the group's next S, in the place of the P that was just used (products are done in order)
+                        const int ahead = i + (kMT == 2 ? 1 : 2);
+                        if (ahead <= last) {
+                            if ((kMT == 1 || g == 0) && !(ok = key_tile())) break;
+                            scores(g, ahead);
+                            if (kMT == 1 || g == 1) step_next();
                         }
                     }
                     if (++stage == M::kStages) stage = 0, ++round;
@@ -374,13 +411,14 @@ __global__ void __launch_bounds__(kThreadsOf[kMT], 1) tree_attention_kernel(cons
         __syncwarp();
     } else if (warp >= 4) {
         // ---- softmax: a thread per row
-        const int m = (warp - 4) / 4;
+        const int g = (warp - 4) / 4, m = kMT == 2 ? g : 0;  // group, tile of rows
         const int row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t sp = tmem + g * 128 + lanes, op = tmem + 256 + g * 128 + lanes;
+        constexpr int kStep = kMT == 2 ? 1 : 2;  // between tiles of a group
         int stage = 0;
-        unsigned round = 0, s_phase[2] = {0, 0}, o_count = 0;
+        unsigned round = 0, tiles = 0, halves = 0;
         bool ok = true;
-        int sbuf = kMT == 1 ? 0 : m;
         const long long range_start = left;  // (a segment that begins here is the piece's first)
         const int node_in = row / P.G;
         const int head_in = row - node_in * P.G;
@@ -394,15 +432,15 @@ __global__ void __launch_bounds__(kThreadsOf[kMT], 1) tree_attention_kernel(cons
             float top = DSSD_NEG_INF, sum = 0.f;  // the maximum that weights refer to, in units of S
             uint32_t sees[4] = {0, 0, 0, 0};      // the row's node's ancestors and itself
             bool no_key = false;                  // there is no node `row`
-            if (at.tile == 0) {
-                short *const parent = S.parent[warp - 4];
+            if (at.tile == 0 && (kMT == 2 || g == 0)) {
+                signed char *const parent = S.parent[warp - 4];
                 bool bad = false;
                 __syncwarp();
                 for (int j = lane; j < P.N; j += 32) {
                     int p = j - 1;
                     if (j > 0 && P.parents) p = ld_after(P.parents + at.b * (P.N - 1) + j - 1);
                     bad |= j > 0 && p >= j;
-                    parent[j] = (short)(j == 0 ? 0 : p >= j ? -1 : max(p, -1));
+                    parent[j] = (signed char)(j == 0 ? 0 : p >= j ? -1 : max(p, -1));
                 }
                 __syncwarp();
                 if (in_tile) {
@@ -427,153 +465,196 @@ __global__ void __launch_bounds__(kThreadsOf[kMT], 1) tree_attention_kernel(cons
                 }
                 if (bad && h == 0 && rt == 0 && m == 0 && P.flags) atomicOr(P.flags + at.b, DSSD_CACHE_FLAG_BAD_NODE);
             }
-            for (int i = at.tile; i < at.tile + n; ++i) {
-                if (!(ok = warp_wait(&S.s_full[sbuf], s_phase[sbuf], failed))) break;
-                s_phase[sbuf] ^= 1;
-                tc_after();
-                const int valid = i == 0 ? P.N : min(kTile, at.ctx - (i - 1) * kTile);
-                const int parts = (valid + 31) / 32;
-                const uint32_t sp = tmem + sbuf * 128 + lanes;
-                // which of 32 columns count
-                auto allowed = [&](int part) {
-                    const uint32_t s = part == 0 ? sees[0] : part == 1 ? sees[1] : part == 2 ? sees[2] : sees[3];
-                    const int v = valid - part * 32;
-                    return (i == 0 ? s : 0xffffffffu) & (v >= 32 ? 0xffffffffu : (1u << v) - 1u);
-                };
-                const bool masked = i == 0 || valid < kTile;
-                float hi = DSSD_NEG_INF;
-                for (int part = 0; part < parts; ++part) {
-                    uint32_t s[32];
-                    tmem_ld32(sp + part * 32, s);
-                    tmem_ld_wait();
-                    if (masked) {
-                        const uint32_t a = allowed(part);
-#pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            if ((a >> k) & 1u) hi = fmaxf(hi, __uint_as_float(s[k]));
-                    } else {
-                        float h4[4] = {DSSD_NEG_INF, DSSD_NEG_INF, DSSD_NEG_INF, DSSD_NEG_INF};
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) h4[k & 3] = fmaxf(h4[k & 3], __uint_as_float(s[k]));
-                        hi = fmaxf(hi, fmaxf(fmaxf(h4[0], h4[1]), fmaxf(h4[2], h4[3])));
-                    }
-                }
-                const bool begin = i == at.tile;
-                bool o_known = begin;
-                const bool raise = hi > top && (hi - top) * P.c > 8.f;  // (top = -inf: the first keys that count)
-                if (__any_sync(0xffffffffu, raise)) {
-                    const float f = raise ? (top == DSSD_NEG_INF ? 0.f : ex2((top - hi) * P.c)) : 1.f;
-                    if (raise) top = hi;
-                    sum *= f;
-                    if (!begin) {
-                        if (!(ok = warp_wait(&S.o_done[m], (o_count - 1) & 1, failed))) break;
-                        o_known = true;
-                        tc_after();
-                        for (int x = 0; x < DP; x += 32) {
-                            uint32_t o[32];
-                            tmem_ld32(tmem + 256 + m * 128 + lanes + x, o);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                            tmem_st32(tmem + 256 + m * 128 + lanes + x, o);
-                        }
-                    }
-                }
-                const float ref = top == DSSD_NEG_INF ? 0.f : -top * P.c;
-                const f32x2 c2 = pack2(P.c, P.c), ref2 = pack2(ref, ref);
-                f32x2 part_sum = pack2(0.f, 0.f);
-                for (int part = 0; part < parts; ++part) {
-                    uint32_t s[32], p[16];
-                    tmem_ld32(sp + part * 32, s);
-                    tmem_ld_wait();
-                    if (masked) {
-                        const uint32_t a = allowed(part);
+            bool begin = true;
+            for (int x = 0; x < n; ++x) {
+                if (kStep == 1 || (x & 1) == g) {
+                    const int i = at.tile + x;
+                    if (!(ok = warp_wait(&S.s_full[g], tiles & 1, failed))) break;
+                    tc_after();
+                    const int valid = i == 0 ? P.N : min(kTile, at.ctx - (i - 1) * kTile);
+                    const bool masked = i == 0 || valid < kTile;
+                    // columns that do not count become -inf
+                    auto mask = [&](uint32_t (&s)[32], int part) {
+                        const int v = valid - part * 32;
+                        const uint32_t a = (i == 0 ? sees[part] : 0xffffffffu) & (v >= 32 ? 0xffffffffu : v > 0 ? (1u << v) - 1u : 0u);
 #pragma unroll
                         for (int k = 0; k < 32; ++k)
                             if (!((a >> k) & 1u)) s[k] = 0xff800000u;
-                    }
+                    };
+                    auto most = [&](const uint32_t (&s)[32]) {
+                        float h4[4];
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        float x, y;
-                        unpack2(fma2(pack2(__uint_as_float(s[2 * k]), __uint_as_float(s[2 * k + 1])), c2, ref2), x, y);
-                        x = ex2(x);
-                        y = ex2(y);
-                        part_sum = add2(part_sum, pack2(x, y));
-                        p[k] = pack<DT>(x, y);
+                        for (int k = 0; k < 4; ++k) h4[k] = __uint_as_float(s[k]);
+#pragma unroll
+                        for (int k = 4; k < 32; ++k) h4[k & 3] = fmaxf(h4[k & 3], __uint_as_float(s[k]));
+                        return fmaxf(fmaxf(h4[0], h4[1]), fmaxf(h4[2], h4[3]));
+                    };
+                    // All of S twice, 32 columns at a time and the next on their way: once for the maximum, once for the weights.  (In registers at
+                    // once it would not fit.)
+                    uint32_t sa[32], sb[32], sc[32];
+                    float hi;
+                    tmem_ld32(sp, sa);
+                    tmem_ld_wait(sa);
+                    tmem_ld32(sp + 32, sb);
+                    if (masked) mask(sa, 0);
+                    hi = most(sa);
+                    tmem_ld_wait(sb);
+                    tmem_ld32(sp + 64, sa);
+                    if (masked) mask(sb, 1);
+                    hi = fmaxf(hi, most(sb));
+                    tmem_ld_wait(sa);
+                    tmem_ld32(sp + 96, sb);
+                    if (masked) mask(sa, 2);
+                    hi = fmaxf(hi, most(sa));
+                    tmem_ld_wait(sb);
+                    tmem_ld32(sp, sa);
+                    if (masked) mask(sb, 3);
+                    hi = fmaxf(hi, most(sb));
+                    bool o_known = begin;
+                    const bool raise = hi > top && (hi - top) * P.c > 8.f;  // (top = -inf: the first keys that count)
+                    if (__any_sync(0xffffffffu, raise)) {
+                        const float f = raise ? (top == DSSD_NEG_INF ? 0.f : ex2((top - hi) * P.c)) : 1.f;
+                        if (raise) top = hi;
+                        sum *= f;
+                        if (!begin) {
+                            if (!(ok = warp_wait(&S.o_done[g], (tiles - 1) & 1, failed))) break;
+                            o_known = true;
+                            tc_after();
+#pragma unroll 1
+                            for (int y = 0; y < DP; y += 32) {
+                                uint32_t o[32];
+                                tmem_ld32(op + y, o);
+                                tmem_ld_wait(o);
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                                tmem_st32(op + y, o);
+                            }
+                        }
                     }
-                    tmem_st16(sp + part * 16, p);
-                }
-                float even, odd;
-                unpack2(part_sum, even, odd);
-                sum += even + odd;
-                tmem_st_wait();
-                tc_before();
-                if (masked && m == 0) {
-                    // what lies behind the last key, or belongs to no node, is made zero: its weight is, but zero times NaN is not
-                    if (!(ok = warp_wait(&S.v_full[stage], round & 1, failed))) break;
-                    const int upto = (valid + 15) / 16 * 16;
-                    if (row < upto && (row >= valid || (i == 0 && no_key))) {
-                        unsigned char *v = base + M::kKV + stage * 2 * M::kOperand + M::kOperand + row * 128;
-                        for (int x = 0; x < kChunks; ++x)
-                            for (int y = 0; y < 128; y += 16) *reinterpret_cast<uint4 *>(v + x * M::kChunk + y) = make_uint4(0, 0, 0, 0);
+                    const float ref = top == DSSD_NEG_INF ? 0.f : -top * P.c;
+                    const f32x2 c2 = pack2(P.c, P.c), ref2 = pack2(ref, ref);
+                    f32x2 part_sum[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+                    auto weigh = [&](const uint32_t (&s)[32], int part) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            float u, v;
+                            unpack2(fma2(pack2(__uint_as_float(s[2 * k]), __uint_as_float(s[2 * k + 1])), c2, ref2), u, v);
+                            u = ex2(u);
+                            v = ex2(v);
+                            part_sum[k & 1] = add2(part_sum[k & 1], pack2(u, v));
+                            p[k] = pack<DT>(u, v);
+                        }
+                        tmem_st16(sp + part * 16, p);
+                    };
+                    // (P of 32 columns takes the place of 16 columns of S that have been read)
+                    tmem_ld_wait(sa);
+                    tmem_ld32(sp + 32, sc);
+                    if (masked) mask(sa, 0);
+                    weigh(sa, 0);
+                    tmem_ld_wait(sc);
+                    tmem_ld32(sp + 64, sa);
+                    if (masked) mask(sc, 1);
+                    weigh(sc, 1);
+                    tmem_ld_wait(sa);
+                    if (masked) mask(sa, 2);
+                    weigh(sa, 2);
+                    weigh(sb, 3);
+                    float even, odd;
+                    unpack2(add2(part_sum[0], part_sum[1]), even, odd);
+                    sum += even + odd;
+                    tmem_st_wait();
+                    tc_before();
+                    if (masked && (kMT == 1 || g == 0)) {
+                        // what lies behind the last key, or belongs to no node, is made zero: its weight is, but zero times NaN is not
+                        if (!(ok = warp_wait(&S.v_full[stage], round & 1, failed))) break;
+                        const int upto = (valid + 15) / 16 * 16;
+                        if (row < upto && (row >= valid || (i == 0 && no_key))) {
+                            unsigned char *v = base + M::kKV + stage * 2 * M::kOperand + M::kOperand + row * 128;
+                            for (int y = 0; y < kChunks; ++y)
+                                for (int z = 0; z < 128; z += 16) *reinterpret_cast<uint4 *>(v + y * M::kChunk + z) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_async();
                     }
-                    fence_async();
+                    // The tile before has to be in O before this one's weights are given away: a barrier tells its last two phases
+                    // apart and no more.  (It is, as a rule.)
+                    if (!o_known && !(ok = warp_wait(&S.o_done[g], (tiles - 1) & 1, failed))) break;
+                    bar_arrive(&S.p_ready[g]);
+                    ++tiles;
+                    begin = false;
                 }
-                // The tile before has to be in O before this one's weights are given away: a barrier tells its last two phases
-                // apart and no more.  (It is, as a rule.)
-                if (!o_known && !(ok = warp_wait(&S.o_done[m], (o_count - 1) & 1, failed))) break;
-                bar_arrive(&S.p_ready[sbuf]);
-                ++o_count;
-                if (kMT == 1) sbuf ^= 1;
                 if (++stage == M::kStages) stage = 0, ++round;
             }
             if (!ok) {
                 if (P.flags) atomicOr(P.flags + at.b, DSSD_CACHE_FLAG_TIMEOUT);
                 break;
             }
-            if (!(ok = warp_wait(&S.o_done[m], (o_count - 1) & 1, failed))) break;
+            const bool mine = !begin;  // this group had keys of the item (with one tile of it the second had none)
+            if (mine && !(ok = warp_wait(&S.o_done[g], (tiles - 1) & 1, failed))) break;
             tc_after();
-            const bool whole = n == at.tiles;
-            if (whole) {
-                const float inv = 1.f / sum;
+            const bool two = kMT == 1 && n > 1;
+            float w0 = 1.f, w1 = 0.f;
+            if (two) {
+                if (g == 1) {
+                    S.other[row] = make_float2(top, sum);
+                    tc_before();
+                    bar_arrive(&S.half);
+                } else {
+                    if (!(ok = warp_wait(&S.half, halves & 1, failed))) break;
+                    tc_after();
+                    const float2 ml = S.other[row];
+                    const float t2 = fmaxf(top, ml.x), r = t2 == DSSD_NEG_INF ? 0.f : t2;
+                    w0 = ex2((top - r) * P.c);
+                    w1 = ex2((ml.x - r) * P.c);
+                    sum = sum * w0 + ml.y * w1;
+                    top = t2;
+                }
+                ++halves;
+            }
+            if (kMT == 2 || g == 0) {
+                const bool whole = n == at.tiles;
                 const int head = h * P.G + head_in;
+                const long long r = (2ll * blockIdx.x + (left == range_start ? 0 : 1)) * (kMT * 128) + m * 128 + row;
+                const float inv = 1.f / sum;
+                if (whole) w0 *= inv, w1 *= inv;
                 unsigned short *to = static_cast<unsigned short *>(P.o) + at.b * P.o_b + node * P.o_n + head * P.o_h;
+                float *part = P.part + r * DP;
+#pragma unroll 1
                 for (int x = 0; x < DP; x += 32) {
                     uint32_t o[32];
                     __syncwarp();
-                    tmem_ld32(tmem + 256 + m * 128 + lanes + x, o);
-                    tmem_ld_wait();
-                    if (!there) continue;
+                    tmem_ld32(op + x, o);
+                    if (two) {
+                        uint32_t o1[32];
+                        tmem_ld32(op + 128 + x, o1);
+                        tmem_ld_wait(o);
+                        tmem_ld_wait(o1);
 #pragma unroll
-                    for (int k = 0; k < 32; k += 8) {
-                        if (x + k >= P.D) break;
-                        uint4 w;
-                        w.x = pack<DT>(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv);
-                        w.y = pack<DT>(__uint_as_float(o[k + 2]) * inv, __uint_as_float(o[k + 3]) * inv);
-                        w.z = pack<DT>(__uint_as_float(o[k + 4]) * inv, __uint_as_float(o[k + 5]) * inv);
-                        w.w = pack<DT>(__uint_as_float(o[k + 6]) * inv, __uint_as_float(o[k + 7]) * inv);
-                        *reinterpret_cast<uint4 *>(to + x + k) = w;
+                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * w0 + __uint_as_float(o1[k]) * w1);
+                    } else {
+                        tmem_ld_wait(o);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * w0);
+                    }
+                    if (whole && there) {
+#pragma unroll
+                        for (int k = 0; k < 32; k += 8)
+                            if (x + k < P.D)
+                                *reinterpret_cast<uint4 *>(to + x + k) =
+                                    make_uint4(pack<DT>(__uint_as_float(o[k]), __uint_as_float(o[k + 1])), pack<DT>(__uint_as_float(o[k + 2]), __uint_as_float(o[k + 3])),
+                                               pack<DT>(__uint_as_float(o[k + 4]), __uint_as_float(o[k + 5])), pack<DT>(__uint_as_float(o[k + 6]), __uint_as_float(o[k + 7])));
+                    } else if (!whole && in_tile) {
+#pragma unroll
+                        for (int k = 0; k < 32; k += 4) *reinterpret_cast<uint4 *>(part + x + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                     }
                 }
-                if (there && P.lse) P.lse[(at.b * P.N + node) * (P.Hkv * P.G) + head] = top * P.scale + logf(sum);
-            } else {
-                const long long slot = 2ll * blockIdx.x + (left == range_start ? 0 : 1);
-                const long long r = slot * (kMT * 128) + m * 128 + row;
-                float *to = P.part + r * DP;
-                for (int x = 0; x < DP; x += 32) {
-                    uint32_t o[32];
-                    __syncwarp();
-                    tmem_ld32(tmem + 256 + m * 128 + lanes + x, o);
-                    tmem_ld_wait();
-                    if (!in_tile) continue;
-#pragma unroll
-                    for (int k = 0; k < 32; k += 4) *reinterpret_cast<uint4 *>(to + x + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-                }
+                if (whole && there && P.lse) P.lse[(at.b * P.N + node) * (P.Hkv * P.G) + head] = top * P.scale + logf(sum);
                 // a row without a node is marked by the piece that has tile 0
-                if (in_tile) P.part_ml[r] = make_float2(there ? top * P.c : inf, sum);
+                if (!whole && in_tile) P.part_ml[r] = make_float2(there ? top * P.c : inf, sum);
+                tc_before();
+                bar_arrive(&S.o_free[g]);
+                if (two) bar_arrive(&S.o_free[1]);
             }
-            tc_before();
-            bar_arrive(&S.o_free[m]);
             left -= n;
             advance(P, at);
         }
@@ -592,44 +673,40 @@ __global__ void __launch_bounds__(kThreadsOf[kMT], 1) tree_attention_kernel(cons
     if (warp == 2) tmem_free(tmem, 512);
 }
 
-// Joins the pieces of items that lie in several: a warp per row.
+// Joins the pieces of items that lie in several: a CTA per item and eight rows, a warp per row.
 template <int DT, int DP, int kMT>
 __global__ void __launch_bounds__(kThreads) tree_join_kernel(const __grid_constant__ Geometry P)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int rows = P.nodes_per_tile * P.G;  // of a tile
-    const unsigned groups = (unsigned)((kMT * rows + kWarps - 1) / kWarps);
-    const unsigned group = blockIdx.x % groups, rest = blockIdx.x / groups;
-    const unsigned items = (unsigned)(P.Hkv * P.row_items);
-    const unsigned item = rest % items;
-    const long long b = rest / items;
-    const int h = item / P.row_items, rt = item - h * P.row_items;
-    const int x = (int)(group * kWarps) + warp;
+    const int c = blockIdx.x % kMaxCtas, x = (int)(blockIdx.x / kMaxCtas) * kWarps + warp;
     const int m = x / rows, row = x - m * rows;
-    const int node = (rt * kMT + m) * P.nodes_per_tile + row / P.G;
     pdl_wait();
     pdl_trigger();
+    const uint4 raw = ld_row16(P.joins + c);
+    const int4 join = make_int4((int)raw.x, (int)raw.y, (int)raw.z, (int)raw.w);
+    if (join.x < 0) return;
+    const long long b = join.x;
+    const int h = join.y / P.row_items, rt = join.y - h * P.row_items;
+    const int node = (rt * kMT + m) * P.nodes_per_tile + row / P.G;
     if (m >= kMT || node >= P.N) return;
-    const Line line = measure(P, b, false);
-    const long long tiles = tiles_of(length(P, b));
-    const long long n = pieces(line.total, (unsigned)min((long long)kMaxCtas, line.total));
-    const long long x0 = line.before + item * tiles, x1 = x0 + tiles - 1;
-    const long long c0 = ((x0 + 1) * n - 1) / line.total, c1 = ((x1 + 1) * n - 1) / line.total;
-    if (c0 == c1) return;
-    auto slot_row = [&](long long c) {
-        const bool first = c > c0 || c * line.total / n == x0;
-        return (2 * c + (first ? 0 : 1)) * (kMT * 128) + m * 128 + row;
-    };
-    const float2 head = P.part_ml[slot_row(c0)];
-    if (head.x == __int_as_float(0x7f800000)) return;
+    // the item's pieces: the second half (or all) of the piece before this one, then the beginnings of this one and those after it
+    const int count = join.w - c + 2;
+    auto slot_row = [&](int k) { return (long long)(k == 0 ? join.z : 2 * (c + k - 1)) * (kMT * 128) + m * 128 + row; };
     float top = DSSD_NEG_INF;
-    for (long long c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, P.part_ml[slot_row(c)].x);
+    bool none = false;
+    for (int k = lane; k < count; k += 32) {
+        const float t = P.part_ml[slot_row(k)].x;
+        none |= t == __int_as_float(0x7f800000);
+        top = fmaxf(top, t);
+    }
+    if (__any_sync(0xffffffffu, none)) return;  // there is no node
     top = warp_max(top);
     float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
     const bool mine = lane * 4 < DP;
 #pragma unroll 4
-    for (long long c = c0; c <= c1; ++c) {
-        const long long r = slot_row(c);
+    for (int k = 0; k < count; ++k) {
+        const long long r = slot_row(k);
         const float2 ml = P.part_ml[r];
         const float w = ex2(ml.x - top);
         sum += w * ml.y;
@@ -675,12 +752,14 @@ cudaError_t launch_as(const Geometry &P, unsigned grid, unsigned join_grid, cuda
 {
     typedef Smem<DP, kMT> M;
     static PerContext allowed;
-    const int ok = allowed.get([] { return (int)(cudaFuncSetAttribute(tree_attention_kernel<DT, DP, kMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)M::kBytes) == cudaSuccess); });
+    const int ok = allowed.get([] {
+        return (int)(cudaFuncSetAttribute(tree_attention_kernel<DT, DP, kMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)M::kBytes) == cudaSuccess);
+    });
     if (!ok) {
         const cudaError_t e = cudaGetLastError();
         return e == cudaSuccess ? cudaErrorInvalidConfiguration : e;
     }
-    const cudaError_t e = launch_pdl(tree_attention_kernel<DT, DP, kMT>, grid, kThreadsOf[kMT], stream, P, M::kBytes);
+    const cudaError_t e = launch_pdl(tree_attention_kernel<DT, DP, kMT>, grid, kAttend, stream, P, M::kBytes);
     return e == cudaSuccess ? launch_pdl(tree_join_kernel<DT, DP, kMT>, join_grid, kThreads, stream, P) : e;
 }
 
@@ -699,7 +778,7 @@ size_t tree_attention_workspace(int B, int N, int Hq, int Hkv, int D)
     (void)B, (void)Hkv;
     // (no less for fewer key heads: rows by the query heads, of which each key head has a part)
     const size_t rows = (long long)N * Hq <= 64 ? 128 : 256;
-    return 2 * (size_t)kMaxCtas * rows * ((size_t)padded(D) * 4 + 8);
+    return 2 * (size_t)kMaxCtas * rows * ((size_t)padded(D) * 4 + 8) + (kMaxCtas * sizeof(int4) + 255) / 256 * 256;
 }
 
 cudaError_t tree_attention_launch(TreeAttentionParams &P, int dtype, void *workspace, cudaStream_t stream)
@@ -724,7 +803,10 @@ cudaError_t tree_attention_launch(TreeAttentionParams &P, int dtype, void *works
     if (!ok) return cudaErrorInvalidValue;
     g.block_table = P.block_table;
     g.table_stride = P.table_stride;
-    g.max_pages = P.max_pages, g.num_pages = P.num_pages, g.page_size = P.page_size, g.box = box;
+    g.max_pages = P.max_pages, g.num_pages = P.num_pages, g.page_size = P.page_size;
+    g.box_log = 0;
+    while (1 << g.box_log < box) ++g.box_log;
+    g.tile_pages = kTile / P.page_size, g.tile_rest = kTile % P.page_size;
     g.ctx_len = P.ctx_len, g.parents = P.parents;
     g.B = P.B, g.N = P.N, g.Hkv = P.Hkv, g.G = G, g.D = P.D;
     g.nodes_per_tile = per;
@@ -738,8 +820,8 @@ cudaError_t tree_attention_launch(TreeAttentionParams &P, int dtype, void *works
     const int dp = padded(P.D);
     g.part = static_cast<float *>(workspace);
     g.part_ml = reinterpret_cast<float2 *>(g.part + 2 * (size_t)kMaxCtas * rows * dp);
-    const long long items = (long long)P.B * P.Hkv * g.row_items;
-    const unsigned join = (unsigned)(items * ((mt * per * G + kWarps - 1) / kWarps));
+    g.joins = reinterpret_cast<int4 *>(g.part_ml + 2 * (size_t)kMaxCtas * rows);
+    const unsigned join = (unsigned)kMaxCtas * (unsigned)((mt * per * G + kWarps - 1) / kWarps);
     const bool bf = dtype == DSSD_BF16;
     if (dp == 64) {
         if (mt == 1) return bf ? launch_as<DSSD_BF16, 64, 1>(g, kMaxCtas, join, stream) : launch_as<DSSD_F16, 64, 1>(g, kMaxCtas, join, stream);
