@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         S.failed = 0;
     }
-    if (warp == 2) tmem_alloc(&S.tmem, 512);
+    if (warp == 1) tmem_alloc(&S.tmem, 512);
     if (warp == 0 && lane == 0) {
         prefetch_map(&P.q);
         prefetch_map(&P.k_new);
@@ -231,34 +231,33 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
     Place at = S.place;
     long long left = S.count;
 
-    if (warp == 0) {
-        // ---- copies: every lane brings in boxes of its own
-        constexpr int kAhead = 2;
+    if (warp == 0 || warp == 2) {
+        // ---- copies: Q and K by one warp, V by the other
+        const bool keys = warp == 0;
+        const CUtensorMap *const fresh = keys ? &P.k_new : &P.v_new, *const cache = keys ? &P.k_cache : &P.v_cache;
+        uint64_t *const full_bar = keys ? S.k_full : S.v_full, *const empty_bar = keys ? S.k_empty : S.v_empty;
+        unsigned char *const ring = base + M::kKV + (keys ? 0 : M::kOperand);
         int stage = 0;
         unsigned round = 0, items = 0;
         bool ok = true;
         while (left > 0 && ok) {
             const int h = at.item / P.row_items, rt = at.item - h * P.row_items;
             const int n = (int)(left < at.tiles - at.tile ? left : at.tiles - at.tile);
-            if (items) ok = warp_wait(&S.q_empty, (items - 1) & 1, failed);
-            if (ok && lane == 0) {
-                bar_expect(&S.q_full, (uint32_t)(kMT * kChunks * P.nodes_per_tile * P.G * 128));
-                for (int m = 0; m < kMT; ++m)
-                    for (int x = 0; x < kChunks; ++x)
-                        copy_5d(base + M::kQ + m * M::kOperand + x * M::kChunk, &P.q, &S.q_full, x * 64, 0, h, (rt * kMT + m) * P.nodes_per_tile, (int)at.b);
+            if (keys) {
+                if (items) ok = warp_wait(&S.q_empty, (items - 1) & 1, failed);
+                if (ok && elect()) {
+                    bar_expect(&S.q_full, (uint32_t)(kMT * kChunks * P.nodes_per_tile * P.G * 128));
+                    for (int m = 0; m < kMT; ++m)
+                        for (int x = 0; x < kChunks; ++x)
+                            copy_5d(base + M::kQ + m * M::kOperand + x * M::kChunk, &P.q, &S.q_full, x * 64, 0, h, (rt * kMT + m) * P.nodes_per_tile, (int)at.b);
+                }
+                __syncwarp();
             }
             ++items;
-            // A lane's boxes of a tile are lane, lane + 32, ...: box x % 128/box of the tile's positions, 64 columns number x / (128/box).  Where the box
-            // of the first lies in its page is carried along from tile to tile (a division each time took longer than the copies).
-            const int full = kTile >> P.box_log, mask = full - 1, all = full * kChunks;
-            const int first = at.tile > 0 ? (at.tile - 1) * kTile : 0;
-            int page_at[kAhead], off[kAhead];
-#pragma unroll
-            for (int a = 0; a < kAhead; ++a) {
-                const int p = first + (((lane + 32 * a) & mask) << P.box_log);
-                page_at[a] = p / P.page_size;
-                off[a] = p - page_at[a] * P.page_size;
-            }
+            // Lane y looks up the page of the tile's box y (of its first 32), and where it lies in it, which it carries along from tile to tile (a division
+            // each time took longer than the copies).  One thread issues the copies.
+            const int first = (at.tile > 0 ? (at.tile - 1) * kTile : 0) + (lane << P.box_log);
+            int page_at = first / P.page_size, off = first - page_at * P.page_size;
             const int32_t *table = P.block_table + at.b * P.table_stride;
             auto number = [&](int p) {
                 int pg = ld_after(table + p);
@@ -269,146 +268,149 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
                 return pg;
             };
             for (int i = at.tile; ok && i < at.tile + n; ++i) {
-                unsigned char *k = base + M::kKV + stage * 2 * M::kOperand, *v = k + M::kOperand;
+                unsigned char *const to = ring + stage * 2 * M::kOperand;
+                uint64_t *const bar = full_bar + stage;
                 const int pos = (i - 1) * kTile;
                 const int valid = i == 0 ? P.N : min(kTile, at.ctx - pos);
                 const int boxes = (valid + (1 << P.box_log) - 1) >> P.box_log;  // of the cache's tiles
-                const uint32_t bytes = (uint32_t)(kChunks * 128 * (i == 0 ? P.N : boxes << P.box_log));
-                int page[kAhead];
-                if (i > 0)  // the pages are looked up before the wait for the stage
-#pragma unroll
-                    for (int a = 0; a < kAhead; ++a)
-                        if (lane + 32 * a < all && ((lane + 32 * a) & mask) < boxes) page[a] = number(page_at[a]);
-                ok = warp_wait(&S.k_empty[stage], (round & 1) ^ 1, failed);
+                int page = 0, place = off;
+                if (i > 0 && lane < boxes) page = number(page_at);  // before the wait for the stage
+                ok = warp_wait(empty_bar + stage, (round & 1) ^ 1, failed);
                 if (!ok) break;
-                if (lane == 0) bar_expect(&S.k_full[stage], bytes);
-                __syncwarp();
-                auto bring = [&](unsigned char *to, const CUtensorMap *fresh, const CUtensorMap *cache, uint64_t *bar) {
-                    if (i == 0) {
-                        if (lane < kChunks) copy_4d(to + lane * M::kChunk, fresh, bar, lane * 64, h, 0, (int)at.b);
-                        return;
-                    }
+                const bool one = elect();
+                if (one) bar_expect(bar, (uint32_t)(kChunks * 128 * (i == 0 ? P.N : boxes << P.box_log)));
+                if (i == 0) {
+                    if (one)
+                        for (int x = 0; x < kChunks; ++x) copy_4d(to + x * M::kChunk, fresh, bar, x * 64, h, 0, (int)at.b);
+                } else {
+                    for (int y0 = 0; y0 < boxes; y0 += 32) {
+                        if (y0 > 0 && y0 + lane < boxes) {  // (pages of less than four positions)
+                            const int p = pos + ((y0 + lane) << P.box_log);
+                            page = number(p / P.page_size), place = p % P.page_size;
+                        }
+#pragma unroll 4
+                        for (int y = 0; y < 32; ++y) {
+                            if (y0 + y >= boxes) break;
+                            const int pg = __shfl_sync(0xffffffffu, page, y), of = __shfl_sync(0xffffffffu, place, y);
+                            unsigned char *const at_box = to + ((y0 + y) << (P.box_log + 7));
+                            if (one)
 #pragma unroll
-                    for (int a = 0; a < kAhead; ++a) {
-                        const int x = lane + 32 * a, y = x & mask;
-                        const int chunk = kChunks == 1 ? 0 : x >= full;
-                        if (x < all && y < boxes) copy_4d(to + chunk * M::kChunk + (y << P.box_log) * 128, cache, bar, chunk * 64, h, off[a], page[a]);
+                                for (int x = 0; x < kChunks; ++x) copy_4d(at_box + x * M::kChunk, cache, bar, x * 64, h, of, pg);
+                        }
                     }
-                    for (int x = lane + 32 * kAhead; x < all; x += 32) {  // (pages of less than four positions)
-                        const int y = x & mask, chunk = kChunks == 1 ? 0 : x >= full, p = pos + (y << P.box_log);
-                        if (y < boxes) copy_4d(to + chunk * M::kChunk + (y << P.box_log) * 128, cache, bar, chunk * 64, h, p % P.page_size, number(p / P.page_size));
-                    }
-                };
-                bring(k, &P.k_new, &P.k_cache, &S.k_full[stage]);
-                ok = warp_wait(&S.v_empty[stage], (round & 1) ^ 1, failed);
-                if (!ok) break;
-                if (lane == 0) bar_expect(&S.v_full[stage], bytes);
+                    // 128 positions on
+                    page_at += P.tile_pages;
+                    off += P.tile_rest;
+                    if (off >= P.page_size) off -= P.page_size, ++page_at;
+                }
                 __syncwarp();
-                bring(v, &P.v_new, &P.v_cache, &S.v_full[stage]);
-                if (i > 0)
-#pragma unroll
-                    for (int a = 0; a < kAhead; ++a) {  // 128 positions on
-                        page_at[a] += P.tile_pages;
-                        off[a] += P.tile_rest;
-                        if (off[a] >= P.page_size) off[a] -= P.page_size, ++page_at[a];
-                    }
                 if (++stage == M::kStages) stage = 0, ++round;
             }
             left -= n;
             advance(P, at);
         }
     } else if (warp == 1) {
-        // ---- products, issued by one thread
-        if (lane == 0) {
-            int stage = 0, next = 0;  // of PV, of QK
-            unsigned round = 0, next_round = 0, items = 0;
-            unsigned p_phase[2] = {0, 0}, uses[2] = {0, 0};
-            bool ok = true;
-            const uint64_t q_operand = operand(smem_u32(base + M::kQ), 16, 1024), k_operand = operand(smem_u32(base + M::kKV), 16, 1024);
-            const uint64_t v_operand = operand(smem_u32(base + M::kKV + M::kOperand), M::kChunk, 1024);
-            while (left > 0 && ok) {
-                const int n = (int)(left < at.tiles - at.tile ? left : at.tiles - at.tile);
-                ok = bar_wait(&S.q_full, items & 1, failed);
-                if (!ok) break;
-                auto valid_of = [&](int i) { return i == 0 ? P.N : min(kTile, at.ctx - (i - 1) * kTile); };
-                // Operands step by adding to the low word of their descriptors (a place in shared memory, by 16 bytes; it never carries): made
-                // anew for every product they took longer than the products.
-                // S of group g for the tile of keys i
-                auto scores = [&](int g, int i) {
-                    const uint64_t q = q_operand + (kMT == 2 ? g * (M::kOperand >> 4) : 0), k = k_operand + next * (2 * M::kOperand >> 4);
-                    const int valid = valid_of(i);
-                    const uint32_t sh = valid == kTile ? shape<DT == DSSD_BF16>(128, 128, false) : shape<DT == DSSD_BF16>(128, (valid + 15) / 16 * 16, false);
+        // ---- products: the warp goes through the tiles together and one thread issues, so that operands stay in uniform registers
+        int stage = 0, next = 0;  // of PV, of QK
+        unsigned round = 0, next_round = 0, items = 0;
+        unsigned p_phase[2] = {0, 0}, uses[2] = {0, 0};
+        bool ok = true;
+        const uint64_t q_operand = operand(smem_u32(base + M::kQ), 16, 1024), k_operand = operand(smem_u32(base + M::kKV), 16, 1024);
+        const uint64_t v_operand = operand(smem_u32(base + M::kKV + M::kOperand), M::kChunk, 1024);
+        const bool one = elect();
+        while (left > 0 && ok) {
+            const int n = (int)(left < at.tiles - at.tile ? left : at.tiles - at.tile);
+            ok = warp_wait(&S.q_full, items & 1, failed);
+            if (!ok) break;
+            auto valid_of = [&](int i) { return i == 0 ? P.N : min(kTile, at.ctx - (i - 1) * kTile); };
+            // Operands step by adding to the low word of their descriptors (a place in shared memory, by 16 bytes; it never carries): made
+            // anew for every product they took longer than the products.
+            // S of group g for the tile of keys i
+            auto scores = [&](int g, int i) {
+                const uint64_t q = q_operand + (kMT == 2 ? g * (M::kOperand >> 4) : 0), k = k_operand + next * (2 * M::kOperand >> 4);
+                const int valid = valid_of(i);
+                const uint32_t sh = valid == kTile ? shape<DT == DSSD_BF16>(128, 128, false) : shape<DT == DSSD_BF16>(128, (valid + 15) / 16 * 16, false);
+                if (one) {
 #pragma unroll
                     for (int x = 0; x < DP / 16; ++x) {
                         const uint32_t in = ((x / 4) * M::kChunk + (x % 4) * 32) >> 4;
                         mma_ss(tmem + g * 128, q + in, k + in, sh, x > 0);
                     }
                     mma_commit(&S.s_full[g]);
-                };
-                auto outputs = [&](int g, int i, bool add) {
-                    const uint64_t v = v_operand + stage * (2 * M::kOperand >> 4);
-                    constexpr uint32_t sh = shape<DT == DSSD_BF16>(128, DP, true);
-                    const int steps = (valid_of(i) + 15) / 16;
-                    const uint32_t o = tmem + 256 + g * 128, p = tmem + g * 128;
-#pragma unroll
-                    for (int x = 0; x < 8; ++x)
-                        if (x < steps) mma_ts(o, p + x * 8, v + x * (2048 >> 4), sh, add || x > 0);
-                    mma_commit(&S.o_done[g]);
-                };
-                auto step_next = [&]() {
-                    mma_commit(&S.k_empty[next]);
-                    if (++next == M::kStages) next = 0, ++next_round;
-                };
-                auto key_tile = [&]() {
-                    const bool there = bar_wait(&S.k_full[next], next_round & 1, failed);
-                    tc_after();
-                    return there;
-                };
-                const int first = at.tile, last = at.tile + n - 1;
-                // the S that need no P before them
-                if (kMT == 2) {
-                    if (!(ok = key_tile())) break;
-                    scores(0, first);
-                    scores(1, first);
-                    step_next();
-                } else
-                    for (int g = 0; g < 2 && g < n && ok; ++g) {
-                        if (!(ok = key_tile())) break;
-                        scores(g, first + g);
-                        step_next();
-                    }
-                for (int i = first; i <= last && ok; ++i) {
-                    for (int g = kMT == 2 ? 0 : (i - first) & 1; g < 2 && ok; g += kMT == 2 ? 1 : 2) {
-                        const bool begin = i - first < (kMT == 2 ? 1 : 2);  // the group's first tile of this item
-                        if (!(ok = bar_wait(&S.p_ready[g], p_phase[g], failed))) break;
-                        p_phase[g] ^= 1;
-                        if ((kMT == 1 || g == 0) && !(ok = bar_wait(&S.v_full[stage], round & 1, failed))) break;
-                        if (begin) {
-                            if (uses[g] && !(ok = bar_wait(&S.o_free[g], (uses[g] - 1) & 1, failed))) break;
-                            ++uses[g];
-                        }
-                        tc_after();
-                        outputs(g, i, !begin);
-                        if (kMT == 1 || g == 1) mma_commit(&S.v_empty[stage]);
-                        // the group's next S, in the place of the P that was just used (products are done in order)
-                        const int ahead = i + (kMT == 2 ? 1 : 2);
-                        if (ahead <= last) {
-                            if ((kMT == 1 || g == 0) && !(ok = key_tile())) break;
-                            scores(g, ahead);
-                            if (kMT == 1 || g == 1) step_next();
-                        }
-                    }
-                    if (++stage == M::kStages) stage = 0, ++round;
                 }
-                if (ok) mma_commit(&S.q_empty);
-                ++items;
-                left -= n;
-                advance(P, at);
+                __syncwarp();
+            };
+            auto outputs = [&](int g, int i, bool add) {
+                const uint64_t v = v_operand + stage * (2 * M::kOperand >> 4);
+                constexpr uint32_t sh = shape<DT == DSSD_BF16>(128, DP, true);
+                const int steps = (valid_of(i) + 15) / 16;
+                const uint32_t o = tmem + 256 + g * 128, p = tmem + g * 128;
+                if (one) {
+                    if (steps == 8) {
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) mma_ts(o, p + x * 8, v + x * (2048 >> 4), sh, add || x > 0);
+                    } else
+                        for (int x = 0; x < steps; ++x) mma_ts(o, p + x * 8, v + x * (2048 >> 4), sh, add || x > 0);
+                    mma_commit(&S.o_done[g]);
+                }
+                __syncwarp();
+            };
+            auto commit = [&](uint64_t *bar) {
+                if (one) mma_commit(bar);
+                __syncwarp();
+            };
+            auto step_next = [&]() {
+                commit(&S.k_empty[next]);
+                if (++next == M::kStages) next = 0, ++next_round;
+            };
+            auto key_tile = [&]() {
+                const bool there = warp_wait(&S.k_full[next], next_round & 1, failed);
+                tc_after();
+                return there;
+            };
+            const int first = at.tile, last = at.tile + n - 1;
+            // the S that need no P before them
+            if (kMT == 2) {
+                if (!(ok = key_tile())) break;
+                scores(0, first);
+                scores(1, first);
+                step_next();
+            } else
+                for (int g = 0; g < 2 && g < n && ok; ++g) {
+                    if (!(ok = key_tile())) break;
+                    scores(g, first + g);
+                    step_next();
+                }
+            for (int i = first; i <= last && ok; ++i) {
+                for (int g = kMT == 2 ? 0 : (i - first) & 1; g < 2 && ok; g += kMT == 2 ? 1 : 2) {
+                    const bool begin = i - first < (kMT == 2 ? 1 : 2);  // the group's first tile of this item
+                    if (!(ok = warp_wait(&S.p_ready[g], p_phase[g], failed))) break;
+                    p_phase[g] ^= 1;
+                    if ((kMT == 1 || g == 0) && !(ok = warp_wait(&S.v_full[stage], round & 1, failed))) break;
+                    if (begin) {
+                        if (uses[g] && !(ok = warp_wait(&S.o_free[g], (uses[g] - 1) & 1, failed))) break;
+                        ++uses[g];
+                    }
+                    tc_after();
+                    outputs(g, i, !begin);
+                    if (kMT == 1 || g == 1) commit(&S.v_empty[stage]);
+                    // the group's next S, in the place of the P that was just used (products are done in order)
+                    const int ahead = i + (kMT == 2 ? 1 : 2);
+                    if (ahead <= last) {
+                        if ((kMT == 1 || g == 0) && !(ok = key_tile())) break;
+                        scores(g, ahead);
+                        if (kMT == 1 || g == 1) step_next();
+                    }
+                }
+                if (++stage == M::kStages) stage = 0, ++round;
             }
-            // the last arrival that the tensor core owes this CTA's shared memory
-            if (ok && items) bar_wait(&S.q_empty, (items - 1) & 1, failed);
+            if (ok) commit(&S.q_empty);
+            ++items;
+            left -= n;
+            advance(P, at);
         }
-        __syncwarp();
+        // the last arrival that the tensor core owes this CTA's shared memory
+        if (ok && items) warp_wait(&S.q_empty, (items - 1) & 1, failed);
     } else if (warp >= 4) {
         // ---- softmax: a thread per row
         const int g = (warp - 4) / 4, m = kMT == 2 ? g : 0;  // group, tile of rows
@@ -670,7 +672,7 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
                     ;
         __syncthreads();
     }
-    if (warp == 2) tmem_free(tmem, 512);
+    if (warp == 1) tmem_free(tmem, 512);
 }
 
 // Joins the pieces of items that lie in several: a CTA per item and eight rows, a warp per row.
