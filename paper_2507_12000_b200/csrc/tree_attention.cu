@@ -35,7 +35,7 @@ namespace {
 constexpr int kTile = 128;      // keys of a tile, rows of a tile
 constexpr int kMaxCtas = 148;   // pieces of the line
 constexpr int kMinTiles = 2;    // tiles to a piece at least
-constexpr int kAttend = 384;     // threads: copies, products and two idle warps; the two groups of the softmax
+constexpr int kAttend = 384;     // threads: copies, products and an idle warp; the two groups of the softmax
 
 struct Geometry {
     CUtensorMap q, k_new, v_new, k_cache, v_cache;
@@ -85,6 +85,12 @@ __device__ __forceinline__ long long pieces(long long total, unsigned grid)
     return n < (long long)grid ? n : (long long)grid;
 }
 
+// a / b of numbers that are small as a rule
+__device__ __forceinline__ long long quotient(long long a, long long b)
+{
+    return ((a | b) >> 32) == 0 ? (long long)((unsigned)a / (unsigned)b) : a / b;
+}
+
 // where a piece of the line begins
 struct Place {
     long long b;
@@ -114,7 +120,7 @@ __device__ Place find(const Geometry &P, long long at)  // one warp, all lanes g
             r.b = i0 + l;
             r.tiles = __shfl_sync(0xffffffffu, t, l);
             r.ctx = __shfl_sync(0xffffffffu, ctx, l);
-            r.item = (int)((at - start) / r.tiles);
+            r.item = (int)quotient(at - start, r.tiles);
             r.tile = (int)((at - start) - (long long)r.item * r.tiles);
             return r;
         }
@@ -209,7 +215,7 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
         const long long total = measure(P, blockIdx.x == 0), c = blockIdx.x;
         const long long n = pieces(total, gridDim.x);
         long long from = 0, to = 0;
-        if (c < n) from = c * total / n, to = (c + 1) * total / n;
+        if (c < n) from = quotient(c * total, n), to = quotient((c + 1) * total, n);
         Place p = {0, 0, 0, 1, 0};
         if (to > from) p = find(P, from);
         if (lane == 0) {
@@ -217,8 +223,8 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
             // an item that begins in the piece before and goes on here is joined under this piece's number
             int4 join = make_int4(-1, 0, 0, 0);
             if (to > from && p.tile > 0) {
-                const long long x0 = from - p.tile, before = (c - 1) * total / n;
-                if (before <= x0) join = make_int4((int)p.b, p.item, 2 * (int)(c - 1) + (before == x0 ? 0 : 1), (int)(((x0 + p.tiles) * n - 1) / total));
+                const long long x0 = from - p.tile, before = quotient((c - 1) * total, n);
+                if (before <= x0) join = make_int4((int)p.b, p.item, 2 * (int)(c - 1) + (before == x0 ? 0 : 1), (int)quotient((x0 + p.tiles) * n - 1, total));
             }
             P.joins[c] = join;
         }
@@ -492,7 +498,7 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
                         return fmaxf(fmaxf(h4[0], h4[1]), fmaxf(h4[2], h4[3]));
                     };
                     // All of S twice, 32 columns at a time and the next on their way: once for the maximum, once for the weights.  (In registers at
-                    // once it would not fit.)
+                    // once, with the warps' registers shared out anew for it, it took as long.)
                     uint32_t sa[32], sb[32], sc[32];
                     float hi;
                     tmem_ld32(sp, sa);
@@ -823,7 +829,7 @@ cudaError_t tree_attention_launch(TreeAttentionParams &P, int dtype, void *works
     g.part = static_cast<float *>(workspace);
     g.part_ml = reinterpret_cast<float2 *>(g.part + 2 * (size_t)kMaxCtas * rows * dp);
     g.joins = reinterpret_cast<int4 *>(g.part_ml + 2 * (size_t)kMaxCtas * rows);
-    const unsigned join = (unsigned)kMaxCtas * (unsigned)((mt * per * G + kWarps - 1) / kWarps);
+    const unsigned join = (unsigned)kMaxCtas * (unsigned)(((P.N < mt * per ? P.N : mt * per) * G + kWarps - 1) / kWarps);
     const bool bf = dtype == DSSD_BF16;
     if (dp == 64) {
         if (mt == 1) return bf ? launch_as<DSSD_BF16, 64, 1>(g, kMaxCtas, join, stream) : launch_as<DSSD_F16, 64, 1>(g, kMaxCtas, join, stream);
