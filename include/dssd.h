@@ -600,12 +600,17 @@ dssd_status dssd_resample_shard_draw(const double *masses, int G, int g, int v_b
  */
 #define DSSD_TREE_MAX_NODES 128
 
+#define DSSD_ADJUST_MAX_V (1 << 24) /* of dssd_adjust_logits */
+
 /* flags written by dssd_adjust_logits, one word per sequence */
 #define DSSD_ADJUST_FLAG_BAD_TOKEN 1u  /* a token of the history, the draft or the biases is outside [0, V): it counts for nothing */
 #define DSSD_ADJUST_FLAG_BAD_PARENT 2u /* see above */
 #define DSSD_ADJUST_FLAG_BAD_LENGTH 4u /* history_len outside [0, history width]: taken as the nearer end */
 #define DSSD_ADJUST_FLAG_BAD_VALUE 8u  /* a repetition penalty that is not a positive finite number: taken as 1 */
 #define DSSD_ADJUST_FLAG_BAD_MASK 16u  /* mask_row beyond the last mask: the row is not masked */
+
+/* Bytes of scratch that dssd_adjust_logits needs (0 if the sizes are invalid). */
+size_t dssd_adjust_logits_workspace_bytes(int B, int N, int V, int L, int K);
 
 /*
  * Penalties for repeated tokens, biases and masks on the N rows of target logits of each sequence (chain: the
@@ -632,6 +637,7 @@ dssd_status dssd_resample_shard_draw(const double *masses, int G, int g, int v_b
  *               stride) works in place and touches only the entries that change.  Rows without a node are left
  *               as they were.  Otherwise the two must not overlap.
  * flags         [B] uint32 out, optional (NULL ok)
+ * workspace     >= dssd_adjust_logits_workspace_bytes(B, N, V, L, K) bytes, 256-byte aligned
  */
 dssd_status dssd_adjust_logits(const void *logits, dssd_dtype dtype, int64_t row_stride, int B, int N, int V,
                                const int32_t *draft_tokens, const int32_t *parents,
@@ -639,7 +645,8 @@ dssd_status dssd_adjust_logits(const void *logits, dssd_dtype dtype, int64_t row
                                const int32_t *history_len, const float *repetition, const float *presence,
                                const float *frequency, const int32_t *bias_tokens, const float *bias_values, int K,
                                const uint32_t *mask, int mask_rows, const int32_t *mask_row, void *out,
-                               int64_t out_stride, uint32_t *flags, void *cuda_stream);
+                               int64_t out_stride, uint32_t *flags, void *workspace, size_t workspace_bytes,
+                               void *cuda_stream);
 
 /* flags of dssd_tree_attention and dssd_cache_append, one word per sequence */
 #define DSSD_CACHE_FLAG_BAD_PAGE 1u   /* a page number outside [0, num_pages): attention reads zeros there, append skips the row */

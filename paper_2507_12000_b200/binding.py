@@ -152,7 +152,9 @@ def _load(path: Optional[str] = None) -> ctypes.CDLL:
         c.c_void_p, c.c_size_t, c.c_void_p]
     i, p, i64 = c.c_int, c.c_void_p, c.c_int64
     L.dssd_adjust_logits.restype = i
-    L.dssd_adjust_logits.argtypes = [p, i, i64, i, i, i, p, p, p, i64, i, p, p, p, p, p, p, p, i, p, i, p, p, i64, p, p]
+    L.dssd_adjust_logits.argtypes = [p, i, i64, i, i, i, p, p, p, i64, i, p, p, p, p, p, p, p, i, p, i, p, p, i64, p, p, c.c_size_t, p]
+    L.dssd_adjust_logits_workspace_bytes.restype = c.c_size_t
+    L.dssd_adjust_logits_workspace_bytes.argtypes = [i, i, i, i, i]
     L.dssd_tree_attention_workspace_bytes.restype = c.c_size_t
     L.dssd_tree_attention_workspace_bytes.argtypes = [i, i, i, i, i]
     L.dssd_tree_attention.restype = i
@@ -525,13 +527,18 @@ def dssd_resample_shard_draw(masses: torch.Tensor, g: int, v_begin: int, p_row_s
 # ---- the round on a drafted tree ------------------------------------------------------------------
 
 
+def dssd_adjust_logits_workspace_bytes(B: int, N: int, V: int, L: int, K: int) -> int:
+    return int(lib.dssd_adjust_logits_workspace_bytes(B, N, V, L, K))
+
+
 def dssd_adjust_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = None, prompt_len: Optional[torch.Tensor] = None,
                        history_len: Optional[torch.Tensor] = None, *, draft_tokens: Optional[torch.Tensor] = None,
                        parents: Optional[torch.Tensor] = None, repetition: Optional[torch.Tensor] = None,
                        presence: Optional[torch.Tensor] = None, frequency: Optional[torch.Tensor] = None,
                        bias_tokens: Optional[torch.Tensor] = None, bias_values: Optional[torch.Tensor] = None,
                        mask: Optional[torch.Tensor] = None, mask_row: Optional[torch.Tensor] = None,
-                       out: Optional[Dict[str, torch.Tensor]] = None, stream=None) -> Dict[str, torch.Tensor]:
+                       out: Optional[Dict[str, torch.Tensor]] = None, workspace: Optional[torch.Tensor] = None,
+                       stream=None) -> Dict[str, torch.Tensor]:
     """Penalties, biases and masks on the logits [B, N, V] of N nodes (a chain's gamma+1 positions where parents is None).
     Row j counts the history and the tokens drafted on its own way from the root.  mask: int32 words [rows, (V+31)//32], a set bit allows
     its token; mask_row [B, N] names each row's mask (negative: none).  Returns {"logits", "flags"}; pass
@@ -539,8 +546,12 @@ def dssd_adjust_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = N
     if out is None:
         out = {"logits": torch.zeros_like(logits, memory_format=torch.contiguous_format),
                "flags": torch.empty(logits.shape[0], dtype=torch.int32, device=logits.device)}
+    if workspace is None:
+        B, N, V = logits.shape
+        workspace = _workspace(dssd_adjust_logits_workspace_bytes(B, N, V, 0 if history is None else history.shape[1],
+                                                                  0 if bias_tokens is None else bias_tokens.shape[1]), logits.device)
     st = _marshal.adjust_logits(logits, history, prompt_len, history_len, draft_tokens, parents, repetition, presence, frequency,
-                                bias_tokens, bias_values, mask, mask_row, out, stream)
+                                bias_tokens, bias_values, mask, mask_row, out, workspace, stream)
     if st != DSSD_OK:
         raise DssdError(st, "dssd_adjust_logits")
     return out

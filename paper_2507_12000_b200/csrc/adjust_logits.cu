@@ -1,16 +1,18 @@
 // Penalties for repeated tokens, biases and masks on the rows of logits of a drafted tree: two kernels.
 //
-// The copy (out of place, or where there are masks) passes the rows by vectors of 16 bytes; what a mask bans becomes -inf. It knows nothing
-// of tokens, and is bound by memory.
+// Which entries a penalty or a bias concerns, a few hundred of a row's 10^5, is the same for all rows of a sequence but for the tokens drafted on the
+// row's own way.  The first kernel, a CTA per sequence, counts the sequence's own tokens in a hash table in shared memory (in whole numbers, so that the
+// order of the atomics changes nothing) and leaves a list of them, by buckets of 16384 entries of the vocabulary.  Where a sequence has more tokens
+// than the table holds, the vocabulary is taken in ranges of the table's size, shared out over CTAs, and the table is indexed directly: it cannot overflow either
+// way.  A table over the vocabulary would be 4 V bytes per sequence to clear, fill and read.
 //
-// The patch then writes the entries that a penalty or a bias concerns, a few hundred of a row's 10^5.  Which they are, and how often each
-// occurred, is counted in shared memory in a hash table of the sequence's own tokens: whole numbers, so that the order of the atomics
-// changes nothing.  A table over the vocabulary would be 4 V bytes per sequence to clear, fill and read; counting by slices of the
-// vocabulary in each CTA took 406 us for B=256 N=5 V=151936 in place (9728 CTAs that each read the history), and taking the touched vectors apart
-// on the way made the copy of B=32 N=24 V=128256 issue-bound (141 us).  Where a sequence has more tokens than the table holds, the vocabulary is
-// taken in ranges of the table's size and the table is indexed directly: it cannot overflow either way.
-// The tokens drafted on a row's own way from the root are few and differ from row to row: an entry that is drafted anywhere walks up from its
-// node.
+// The second kernel passes the rows by vectors of 16 bytes (in place: only rows with a mask, and there what the mask bans) and then patches the listed entries
+// of the part that it just wrote, which are in L2 still.  It waits for the list only then: copying and counting run at the same time.
+//
+// In place the patch is a kernel of its own, a CTA to a row.
+//
+// Bound by the copy of the rows, or in place by the entries that change.  Counting by slices of the vocabulary in every CTA of the copy took 141 us for
+// B=32 N=24 V=128256 and 406 for B=256 N=5 V=151936 in place; a patch after the copy that counted for itself 90 and 78.
 #include "launch.h"
 #include "quads.cuh"
 #include "tree.cuh"
@@ -70,6 +72,56 @@ __device__ __forceinline__ const uint32_t *mask_of(const AdjustParams &P, long l
 // ---- the copy --------------------------------------------------------------------------------
 
 constexpr int kCopyVecs = 8;  // of a thread
+constexpr int kBucketLog = 14;
+constexpr uint32_t kInPrompt = 1u << 30, kDrafted = 1u << 31, kCount = kInPrompt - 1;
+
+// An entry of the list: token, occurrences with their flags, place of its bias in the request's list + 1 (0: none), the bias
+__device__ __forceinline__ uint4 list_entry(int v, uint32_t count, unsigned bias, float value) { return make_uint4((uint32_t)v, count, bias, __float_as_uint(value)); }
+
+// What the penalties of a request do to the listed entries of a row
+struct Request {
+    float repetition, presence, frequency;
+    __device__ __forceinline__ Request(const AdjustParams &P, long long b) : repetition(1.f), presence(0.f), frequency(0.f)
+    {
+        if (P.repetition) repetition = ld_after(P.repetition + b);
+        if (P.presence) presence = ld_after(P.presence + b);
+        if (P.frequency) frequency = ld_after(P.frequency + b);
+        if (!(repetition > 0.f && repetition < __int_as_float(0x7f800000))) repetition = 1.f;
+    }
+};
+// The entry that x stands for, in the row of `node`, if it is within [from, to) and not masked: its old value is in `old`
+template <int DT>
+__device__ __forceinline__ void patch(const Request &r, const uint4 &x, typename Vec<DT>::Word old, bool banned, char *out, int node, const short *parent, const int *token)
+{
+    typedef Vec<DT> E;
+    if (banned) return;
+    const int v = (int)x.x;
+    uint32_t n_out = x.y & kCount;
+    if (x.y & kDrafted)
+        for (int j = node; j > 0; j = parent[j]) n_out += token[j] == v;
+    if (!(n_out | (x.y & kInPrompt) | x.z)) return;  // drafted on other ways only
+    float f = E::value(old);
+    if (n_out || (x.y & kInPrompt)) f = f > 0.f ? __fdiv_rn(f, r.repetition) : __fmul_rn(f, r.repetition);
+    if (n_out) f = __fsub_rn(__fsub_rn(f, __fmul_rn(r.frequency, (float)n_out)), r.presence);
+    if (x.z) f = __fadd_rn(f, __uint_as_float(x.w));
+    reinterpret_cast<typename E::Word *>(out)[v] = E::bits(f);
+}
+__device__ __forceinline__ bool banned_by(const uint32_t *mask, int v) { return mask && !((ld_after_u32(mask + (v >> 5)) >> (v & 31)) & 1u); }
+
+// The nodes' parents and tokens in shared memory; whether there is a node `node`.  All threads of the CTA.
+__device__ __forceinline__ bool load_way(const AdjustParams &P, long long b, int node, short *parent, int *token)
+{
+    for (int j = threadIdx.x; j < P.N; j += blockDim.x) {
+        int p = j ? j - 1 : 0;
+        if (P.parents && j) p = ld_after(P.parents + b * (P.N - 1) + j - 1);
+        parent[j] = (short)(p >= j && j ? -1 : max(p, -1));
+        if (j) token[j] = ld_after(P.draft_tokens + b * (P.N - 1) + j - 1);
+    }
+    __syncthreads();
+    int up = node;
+    while (up > 0) up = parent[up];
+    return up == 0;
+}
 
 // kInPlace: only what a mask bans is written.  kVector: a row's entries lie alike to 16 bytes in both arrays.
 template <int DT, bool kInPlace, bool kVector>
@@ -79,22 +131,32 @@ __global__ void __launch_bounds__(kThreads) adjust_copy_kernel(const __grid_cons
     typedef typename E::Word Word;
     constexpr uint32_t kAll = (1u << E::kN) - 1u;
     __shared__ short parent[kMaxNodes];
-    __shared__ int there;
+    __shared__ int token[kMaxNodes];
     const int t = threadIdx.x;
     const long long row = blockIdx.x / (unsigned)P.turns;
     const int turn = blockIdx.x % (unsigned)P.turns;
     const long long b = row / P.N;
     const int node = (int)(row - b * P.N);
-    pdl_wait();
-    pdl_trigger();
+    // The kernel before this one, which makes the list, let this one in when what came before it had ended: all arrays but the list are as they
+    // should be, and the list is waited for below.
     const char *in = static_cast<const char *>(P.logits) + row * P.row_stride * (long long)sizeof(Word);
     char *out = static_cast<char *>(P.out) + row * P.out_stride * (long long)sizeof(Word);
     const uint32_t *mask = mask_of(P, row);
-    if (kInPlace && !mask) return;
+    const uint4 *list = P.list + b * P.list_size;
+    const int2 *buckets = P.buckets + b * P.n_buckets;
     const int words = (P.V + 31) / 32;
     // vectors begin on 16-byte boundaries of memory: the first at most kN - 1 entries before the row
     const int mis = kVector ? (int)((reinterpret_cast<uintptr_t>(in) / sizeof(Word)) % E::kN) : 0;
-    bool known = !P.parents;
+    if (kInPlace) {
+        // The list is not for this kernel, and CTAs that wait for it would stand in the way of those with a mask: one waits, so that this
+        // kernel ends after the one before it.
+        if (blockIdx.x == 0) pdl_wait();
+        if (!mask) return;
+    }
+    if (!load_way(P, b, node, parent, token)) {
+        if (!kInPlace) pdl_wait();
+        return;
+    }
     auto allowed = [&](int v) {
         uint32_t a = kAll;
         if (mask && v + E::kN > 0 && v < P.V) {
@@ -105,8 +167,9 @@ __global__ void __launch_bounds__(kThreads) adjust_copy_kernel(const __grid_cons
         }
         return a;
     };
+    constexpr int kPiece = kThreads * kCopyVecs * E::kN;
     for (int piece = turn; piece < P.pieces; piece += P.turns) {
-        const int v0 = piece * (kThreads * kCopyVecs * E::kN) - mis + t * E::kN;
+        const int v0 = piece * kPiece - mis + t * E::kN;
         uint4 x[kCopyVecs];
         uint32_t a[kCopyVecs];
 #pragma unroll
@@ -118,20 +181,20 @@ __global__ void __launch_bounds__(kThreads) adjust_copy_kernel(const __grid_cons
             // (a vector that is banned altogether is not read, nor in place one that is not banned at all)
             if (kVector && v >= 0 && v + E::kN <= P.V && a[k] && !(kInPlace && a[k] == kAll)) x[k] = ld_row16(in + (long long)v * sizeof(Word));
         }
-        if (!known) {  // is there a node?  (looked up while the row is on its way)
-            for (int j = t; j < P.N; j += kThreads) {
-                const int p = j ? ld_after(P.parents + b * (P.N - 1) + j - 1) : 0;
-                parent[j] = (short)(p >= j && j ? -1 : max(p, -1));
+        // Out of place the listed entries of this part are looked up while the row is on its way (the list is ready but for the first CTAs).
+        const int from = max(piece * kPiece - mis, 0), to = min((piece + 1) * kPiece - mis, P.V);
+        int bucket = from >> kBucketLog, at = 0, end = 0;
+        uint4 x0 = make_uint4(0, 0, 0, 0);
+        if (!kInPlace) {
+            if (piece == turn) {
+                pdl_wait();
+                pdl_trigger();
             }
-            __syncthreads();
-            if (t == 0) {
-                int up = node;
-                while (up > 0) up = parent[up];
-                there = up == 0;
+            if (bucket < P.n_buckets) {
+                const unsigned long long span = ld_after(reinterpret_cast<const unsigned long long *>(buckets + bucket));
+                at = (int)(uint32_t)span + t, end = (int)(span >> 32);
+                if (at < end) x0 = ld_row16(list + at);
             }
-            __syncthreads();
-            if (!there) return;
-            known = true;
         }
 #pragma unroll
         for (int k = 0; k < kCopyVecs; ++k) {
@@ -147,19 +210,79 @@ __global__ void __launch_bounds__(kThreads) adjust_copy_kernel(const __grid_cons
                 else if (!kInPlace) *to = E::load(in + (long long)(v + i) * sizeof(Word));
             }
         }
+        if (!kInPlace) {
+            __syncthreads();  // (an entry is patched by another thread than the one that copied it)
+            const Request r(P, b);
+            for (; bucket <= (to - 1) >> kBucketLog; ++bucket) {
+                if (bucket > from >> kBucketLog) {
+                    const unsigned long long span = ld_after(reinterpret_cast<const unsigned long long *>(buckets + bucket));
+                    at = (int)(uint32_t)span + t, end = (int)(span >> 32);
+                    if (at < end) x0 = ld_row16(list + at);
+                }
+                while (at < end) {
+                    const int v = (int)x0.x;
+                    if (v >= from && v < to) patch<DT>(r, x0, E::load(in + (long long)v * sizeof(Word)), banned_by(mask, v), out, node, parent, token);
+                    at += kThreads;
+                    if (at < end) x0 = ld_row16(list + at);
+                }
+            }
+        }
     }
 }
 
-// ---- the patch -------------------------------------------------------------------------------
+// In place: a CTA patches the listed entries of a row, four requests in flight to a thread.
+template <int DT>
+__global__ void __launch_bounds__(kThreads) adjust_patch_kernel(const __grid_constant__ AdjustParams P)
+{
+    typedef Vec<DT> E;
+    typedef typename E::Word Word;
+    __shared__ short parent[kMaxNodes];
+    __shared__ int token[kMaxNodes];
+    const int t = threadIdx.x;
+    const long long row = blockIdx.x, b = row / P.N;
+    const int node = (int)(row - b * P.N);
+    pdl_wait();
+    pdl_trigger();
+    char *out = static_cast<char *>(P.out) + row * P.out_stride * (long long)sizeof(Word);
+    const uint32_t *mask = mask_of(P, row);
+    const uint4 *list = P.list + b * P.list_size;
+    const unsigned long long *buckets = reinterpret_cast<const unsigned long long *>(P.buckets + b * P.n_buckets);
+    // a hash table's buckets follow one another; those of ranges have gaps between them
+    const int step = P.gaps ? 1 : P.n_buckets;
+    unsigned long long first = ld_after(buckets), last = ld_after(buckets + step - 1);
+    const Request r(P, b);
+    if (!load_way(P, b, node, parent, token)) return;
+    for (int k = 0; k < P.n_buckets; k += step) {
+        if (k) first = last = ld_after(buckets + k);
+        const int end = (int)(last >> 32);
+        for (int e0 = (int)(uint32_t)first + t; e0 < end; e0 += 4 * kThreads) {
+            uint4 x[4];
+            Word old[4];
+            bool banned[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) x[u] = e0 + u * kThreads < end ? ld_row16(list + e0 + u * kThreads) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                banned[u] = e0 + u * kThreads >= end;
+                old[u] = banned[u] ? 0 : E::load(out + (long long)(int)x[u].x * sizeof(Word));
+                if (!banned[u]) banned[u] = banned_by(mask, (int)x[u].x);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) patch<DT>(r, x[u], old[u], banned[u], out, node, parent, token);
+        }
+    }
+}
 
-constexpr int kPatch = 512;  // threads
-constexpr uint32_t kInPrompt = 1u << 30, kDrafted = 1u << 31, kCount = kInPrompt - 1;
+// ---- the list --------------------------------------------------------------------------------
 
-// shared memory: key, count and the last bias (its place in the list + 1) of every slot, then the list of slots in use
+constexpr int kList = 512;  // threads
+constexpr int kMaxBuckets = 1024;
+
+// shared memory: key, count and the last bias (its place in the request's list + 1) of every slot
 struct Table {
     int *key;
     uint32_t *count;
-    unsigned short *bias, *used;
+    unsigned short *bias;
     int slots, first, direct;  // direct: slot = token - first, for tokens first .. first + slots - 1
     __device__ __forceinline__ int find(int v) const
     {
@@ -179,100 +302,99 @@ struct Table {
     }
 };
 
-template <int DT>
-__global__ void __launch_bounds__(kPatch) adjust_patch_kernel(const __grid_constant__ AdjustParams P)
+__global__ void __launch_bounds__(kList) adjust_list_kernel(const __grid_constant__ AdjustParams P)
 {
-    typedef Vec<DT> E;
-    typedef typename E::Word Word;
     extern __shared__ __align__(16) unsigned char raw[];
-    __shared__ int token[kMaxNodes];
     __shared__ short parent[kMaxNodes];
-    __shared__ const uint32_t *masks[kMaxNodes];
-    __shared__ int bad, n_used;
+    __shared__ int bad, start[kMaxBuckets], below;
     __shared__ unsigned all_flags;
-    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    __shared__ float first_values[kList];
+    const int t = threadIdx.x, lane = t & 31;
     const long long b = blockIdx.x / (unsigned)P.shares;
     const int share = blockIdx.x % (unsigned)P.shares;
     Table T;
     T.key = reinterpret_cast<int *>(raw);
     T.count = reinterpret_cast<uint32_t *>(T.key + P.slots);
     T.bias = reinterpret_cast<unsigned short *>(T.count + P.slots);
-    T.used = T.bias + P.slots;
     T.slots = P.slots;
     if (t == 0) all_flags = 0;
-    // After the copy only the logits are waited for: the copy let this kernel in when what came before it had ended, so that all other
-    // arrays are as they should be.
-    bool waited = !P.after_copy;
-    if (waited) {
-        pdl_wait();
-        pdl_trigger();
-    }
-    load_tree(P.parents, b, P.N, parent, &bad);  // (with barriers)
-
-    unsigned flags = bad ? DSSD_ADJUST_FLAG_BAD_PARENT : 0u;
-    float repetition = 1.f, presence = 0.f, frequency = 0.f;
-    if (P.repetition) repetition = ld_after(P.repetition + b);
-    if (P.presence) presence = ld_after(P.presence + b);
-    if (P.frequency) frequency = ld_after(P.frequency + b);
-    if (!(repetition > 0.f && repetition < __int_as_float(0x7f800000))) {
-        repetition = 1.f;
-        flags |= DSSD_ADJUST_FLAG_BAD_VALUE;
-    }
+    pdl_wait();
+    pdl_trigger();
+    // what is needed first is asked for at once, the history as far as it may go
+    const int32_t *hist = P.history + b * P.history_stride;
+    int tok0[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) tok0[u] = t + u * kList < P.L ? ld_after(hist + t + u * kList) : 0;
+    const int bias0 = t < P.K ? ld_after(P.bias_tokens + b * P.K + t) : -1;
+    const float value0 = t < P.K ? ld_after(P.bias_values + b * P.K + t) : 0.f;
     int hl = P.L ? ld_after(P.history_len + b) : 0;
     const int pl = P.L ? ld_after(P.prompt_len + b) : 0;
+    const float r = P.repetition ? ld_after(P.repetition + b) : 1.f;
+    int drafted = t > 0 && t < P.N ? ld_after(P.draft_tokens + b * (P.N - 1) + t - 1) : -1;
+    load_tree(P.parents, b, P.N, parent, &bad);  // (with barriers)
+    first_values[t] = value0;
+
+    unsigned flags = bad ? DSSD_ADJUST_FLAG_BAD_PARENT : 0u;
+    {
+        if (!(r > 0.f && r < __int_as_float(0x7f800000))) flags |= DSSD_ADJUST_FLAG_BAD_VALUE;
+    }
     if (hl < 0 || hl > P.L) {
         hl = hl < 0 ? 0 : P.L;
         flags |= DSSD_ADJUST_FLAG_BAD_LENGTH;
     }
-    if (t < P.N) {
-        masks[t] = mask_of(P, b * P.N + t);
-        if (t > 0) {
-            token[t] = ld_after(P.draft_tokens + b * (P.N - 1) + t - 1);
-            if (parent[t] >= 0 && (token[t] < 0 || token[t] >= P.V)) flags |= DSSD_ADJUST_FLAG_BAD_TOKEN;
+    if (t >= P.N || parent[t] < 0) drafted = -1;
+    else {
+        if (t > 0 && (drafted < 0 || drafted >= P.V)) {
+            drafted = -1;
+            flags |= DSSD_ADJUST_FLAG_BAD_TOKEN;
         }
-        if (P.mask && P.mask_row && parent[t] >= 0 && ld_after(P.mask_row + b * P.N + t) >= P.mask_rows) flags |= DSSD_ADJUST_FLAG_BAD_MASK;
+        if (P.mask && P.mask_row && ld_after(P.mask_row + b * P.N + t) >= P.mask_rows) flags |= DSSD_ADJUST_FLAG_BAD_MASK;
     }
-    // With fewer tokens than three quarters of the slots the table is a hash table of all of them; else the vocabulary is taken in ranges.
+    // With fewer tokens than three quarters of the slots the table is a hash table of all of them; else the vocabulary is taken in ranges of
+    // the largest table, which are buckets.
     T.direct = (long long)hl + P.N + P.K > (long long)T.slots * 3 / 4;
-    const int32_t *hist = P.history + b * P.history_stride;
-    const int ranges = T.direct ? (P.V + T.slots - 1) / T.slots : 1;
-    // the ranges are shared out first, what is in a range (or the one table) by the rows
-    const int r_step = T.direct ? P.shares : 1, p_from = T.direct ? 0 : share, p_step = T.direct ? 1 : P.shares;
-    for (int range = T.direct ? share : 0; range < ranges; range += r_step) {
-        T.first = range * T.slots;
+    uint4 *list = P.list + b * P.list_size;
+    int2 *buckets = P.buckets + b * P.n_buckets;
+    for (int range = T.direct ? share : 0; range < (T.direct ? P.n_buckets : share == 0 ? 1 : 0); range += P.shares) {
+        T.first = range << kBucketLog;
         __syncthreads();
-        for (int i = t; i < T.slots; i += kPatch) T.key[i] = -1, T.count[i] = 0, T.bias[i] = 0;
-        if (t == 0) n_used = 0;
+        for (int i = t; i < T.slots; i += kList) T.key[i] = -1, T.count[i] = 0, T.bias[i] = 0;
+        for (int i = t; i < P.n_buckets && !T.direct; i += kList) start[i] = 0;
+        if (t == 0) below = 0;
         __syncthreads();
+        int under = 0;  // tokens before the range: no more than these have entries before its own
         // in eights: the tokens come from L2, and a request at a time would wait for each
-        for (int i0 = t; i0 < hl; i0 += 8 * kPatch) {
+        for (int i0 = t; i0 < hl; i0 += 8 * kList) {
             int tok[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) tok[u] = i0 + u * kPatch < hl ? ld_after(hist + i0 + u * kPatch) : 0;
+            for (int u = 0; u < 8; ++u) tok[u] = i0 == t ? tok0[u] : i0 + u * kList < hl ? ld_after(hist + i0 + u * kList) : 0;
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                const int i = i0 + u * kPatch;
+                const int i = i0 + u * kList;
                 if (i >= hl) break;
                 if (tok[u] < 0 || tok[u] >= P.V) {
                     flags |= DSSD_ADJUST_FLAG_BAD_TOKEN;
                     continue;
                 }
+                under += tok[u] < T.first;
                 const int s = T.find(tok[u]);
                 if (s < 0) continue;
                 if (i < pl) atomicOr(&T.count[s], kInPrompt);
                 else atomicAdd(&T.count[s], 1u);
             }
         }
-        if (t > 0 && t < P.N && parent[t] >= 0 && token[t] >= 0 && token[t] < P.V) {
-            const int s = T.find(token[t]);
+        if (drafted >= 0) {
+            under += drafted < T.first;
+            const int s = T.find(drafted);
             if (s >= 0) atomicOr(&T.count[s], kDrafted);
         }
         // of a token's biases the last one holds: whoever stores first does not matter, the largest index stays
-        for (int k0 = 0; k0 < P.K; k0 += kPatch) {
+        for (int k0 = 0; k0 < P.K; k0 += kList) {
             const int k = k0 + t;
-            const int v = k < P.K ? ld_after(P.bias_tokens + b * P.K + k) : -1;
+            const int v = k0 == 0 ? bias0 : k < P.K ? ld_after(P.bias_tokens + b * P.K + k) : -1;
             if (v >= P.V) flags |= DSSD_ADJUST_FLAG_BAD_TOKEN;
             const int s = v >= 0 && v < P.V ? T.find(v) : -1;
+            under += v >= 0 && v < T.first;
             bool waiting = s >= 0;
             while (__syncthreads_or(waiting)) {
                 if (waiting) T.bias[s] = (unsigned short)(k + 1);
@@ -280,88 +402,71 @@ __global__ void __launch_bounds__(kPatch) adjust_patch_kernel(const __grid_const
                 if (waiting) waiting = T.bias[s] < (unsigned short)(k + 1);
             }
         }
-        __syncthreads();
-        for (int i = t; i < T.slots; i += kPatch) {  // (slots are a multiple of the threads)
-            const bool in_use = T.key[i] >= 0;
-            const unsigned who = __ballot_sync(0xffffffffu, in_use);
-            int at = 0;
-            if (lane == 0 && who) at = atomicAdd(&n_used, __popc(who));
-            at = __shfl_sync(0xffffffffu, at, 0);
-            if (in_use) T.used[at + __popc(who & ((1u << lane) - 1u))] = (unsigned short)i;
+        if (T.direct) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) under += __shfl_xor_sync(0xffffffffu, under, o);
+            if (lane == 0 && under) atomicAdd(&below, under);
+            if (t == 0) start[range] = 0;
         }
         __syncthreads();
-        if (!waited) {
-            pdl_wait();
-            pdl_trigger();
-            waited = true;
-        }
-        // (entry, row) pairs: a warp takes 256 entries of a row at a time, eight requests in flight to a lane
-        const int n = n_used, blocks = (n + 255) / 256;
-        const int rows = (P.N - p_from + p_step - 1) / p_step;
-        for (int unit = warp; unit < rows * blocks; unit += kPatch / 32) {
-            const int r = unit / blocks, node = p_from + r * p_step;
-            if (parent[node] < 0) continue;
-            const long long row = b * P.N + node;
-            const char *in = static_cast<const char *>(P.logits) + row * P.row_stride * (long long)sizeof(Word);
-            Word *out = static_cast<Word *>(P.out) + row * P.out_stride;
-            const uint32_t *mask = masks[node];
-            constexpr int kAtOnce = 8;
-            const int e0 = (unit - r * blocks) * 256 + lane;
-            int slot[kAtOnce], v[kAtOnce];
-            Word w[kAtOnce];
-            uint32_t allow[kAtOnce];
-#pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) {
-                const int e = e0 + u * 32;
-                slot[u] = e < n ? T.used[e] : -1;
-                v[u] = slot[u] >= 0 ? T.key[slot[u]] : 0;
-                w[u] = slot[u] >= 0 ? E::load(in + (long long)v[u] * sizeof(Word)) : 0;
-                allow[u] = mask && slot[u] >= 0 ? ld_after_u32(mask + (v[u] >> 5)) >> (v[u] & 31) : 1u;
+        // entries to their buckets: how many, where each begins, then the entries (their order within a bucket changes nothing)
+        for (int i = t; i < T.slots; i += kList)
+            if (T.key[i] >= 0) atomicAdd(&start[T.key[i] >> kBucketLog], 1);
+        __syncthreads();
+        if (T.direct) {
+            if (t == 0) {
+                const int n = start[range];
+                start[range] = below;
+                buckets[range] = make_int2(below, below + n);
             }
+        } else if (t < 32) {
+            int base = 0;
+            for (int k0 = 0; k0 < P.n_buckets; k0 += 32) {
+                const int k = k0 + lane, n = k < P.n_buckets ? start[k] : 0;
+                int end = n;
 #pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) {
-                if (slot[u] < 0 || !(allow[u] & 1u)) continue;
-                const uint32_t c = T.count[slot[u]];
-                const unsigned k = T.bias[slot[u]];
-                uint32_t n_out = c & kCount;
-                if (c & kDrafted)
-                    for (int j = node; j > 0; j = parent[j]) n_out += token[j] == v[u];
-                if (!(n_out | (c & kInPrompt) | k)) continue;  // drafted on other ways only
-                float x = E::value(w[u]);
-                if (n_out || (c & kInPrompt)) x = x > 0.f ? __fdiv_rn(x, repetition) : __fmul_rn(x, repetition);
-                if (n_out) x = __fsub_rn(__fsub_rn(x, __fmul_rn(frequency, (float)n_out)), presence);
-                if (k) x = __fadd_rn(x, ld_after(P.bias_values + b * P.K + k - 1));
-                out[v[u]] = E::bits(x);
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int up = __shfl_up_sync(0xffffffffu, end, o);
+                    if (lane >= o) end += up;
+                }
+                if (k < P.n_buckets) {
+                    start[k] = base + end - n;
+                    buckets[k] = make_int2(base + end - n, base + end);
+                }
+                base += __shfl_sync(0xffffffffu, end, 31);
             }
         }
-    }
-    if (!waited) {  // (a share without a range)
-        pdl_wait();
-        pdl_trigger();
+        __syncthreads();
+        for (int i = t; i < T.slots; i += kList) {
+            const int v = T.key[i];
+            if (v < 0) continue;
+            const unsigned k = T.bias[i];
+            list[atomicAdd(&start[v >> kBucketLog], 1)] = list_entry(v, T.count[i], k, !k ? 0.f : k <= kList ? first_values[k - 1] : ld_after(P.bias_values + b * P.K + k - 1));
+        }
     }
     if (share == 0 && P.flags) {
-        // (in ranges, a range sees all tokens; every CTA of the sequence sees the same flags)
+        // (every CTA of the sequence sees all tokens, share 0 at least once)
         flags = __reduce_or_sync(0xffffffffu, flags);
-        if ((t & 31) == 0 && flags) atomicOr(&all_flags, flags);
+        __syncthreads();
+        if (lane == 0 && flags) atomicOr(&all_flags, flags);
         __syncthreads();
         if (t == 0) P.flags[b] = all_flags;
     }
 }
 
-constexpr int kMaxSlots = 16384;
+constexpr int kMaxSlots = 1 << kBucketLog;
 
-template <int DT>
-cudaError_t patch(const AdjustParams &P, cudaStream_t stream)
+cudaError_t make_list(const AdjustParams &P, cudaStream_t stream)
 {
-    const size_t smem = (size_t)P.slots * 12;
+    const size_t smem = (size_t)P.slots * 10;
     if (smem > 40 * 1024) {  // (with what is declared in the kernel, beyond the 48 KB that need no leave)
         static PerContext allowed;
-        if (!allowed.get([] { return (int)(cudaFuncSetAttribute(adjust_patch_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSlots * 12) == cudaSuccess); })) {
+        if (!allowed.get([] { return (int)(cudaFuncSetAttribute(adjust_list_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSlots * 10) == cudaSuccess); })) {
             const cudaError_t e = cudaGetLastError();
             return e == cudaSuccess ? cudaErrorInvalidConfiguration : e;
         }
     }
-    return launch_pdl(adjust_patch_kernel<DT>, (unsigned)P.B * (unsigned)P.shares, kPatch, stream, P, smem);
+    return launch_pdl(adjust_list_kernel, (unsigned)P.B * (unsigned)P.shares, kList, stream, P, smem);
 }
 
 template <int DT, bool kInPlace>
@@ -372,36 +477,62 @@ cudaError_t copy(const AdjustParams &P, bool vector, cudaStream_t stream)
                   : launch_pdl(adjust_copy_kernel<DT, kInPlace, false>, grid, kThreads, stream, P);
 }
 
+// a slot and a third for each token that there may be
+int slots_of(long long tokens)
+{
+    int n = 512;
+    while (n < kMaxSlots && (long long)n * 3 / 4 < tokens) n *= 2;
+    return n;
+}
+size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
+int buckets_of(int V) { return (V + (1 << kBucketLog) - 1) >> kBucketLog; }
+
 }  // namespace
+
+static_assert(DSSD_ADJUST_MAX_V <= kMaxBuckets << kBucketLog, "a counter per bucket");
 
 int adjust_copy_entries(int dtype) { return kThreads * kCopyVecs * (dtype == DSSD_BF16 ? 8 : 4); }
 
-cudaError_t adjust_launch(AdjustParams &P, int dtype, cudaStream_t stream)
+size_t adjust_workspace(int B, int N, int V, int L, int K)
+{
+    return round256((size_t)B * ((size_t)L + N + K) * sizeof(uint4)) + round256((size_t)B * buckets_of(V) * sizeof(int2));
+}
+
+cudaError_t adjust_launch(AdjustParams &P, int dtype, void *workspace, cudaStream_t stream)
 {
     const int esz = dtype == DSSD_BF16 ? 2 : 4;
     const bool in_place = P.out == P.logits, bf = dtype == DSSD_BF16;
+    const long long tokens = (long long)P.L + P.N + P.K;
+    P.list = static_cast<uint4 *>(workspace);
+    P.list_size = tokens;
+    P.buckets = reinterpret_cast<int2 *>(static_cast<char *>(workspace) + round256((size_t)P.B * (size_t)tokens * sizeof(uint4)));
+    P.n_buckets = buckets_of(P.V);
+    P.slots = slots_of(tokens);
+    // tables that may have to be taken in ranges: a few CTAs for these
+    P.shares = 1;
+    if ((long long)P.slots * 3 / 4 < tokens)
+        while (P.shares < P.n_buckets && P.shares < 16 && (long long)P.B * P.shares < 2 * 148) P.shares *= 2;
+    cudaError_t e = make_list(P, stream);
+    if (e != cudaSuccess) return e;
     // a vector store needs the two rows at the same place of a 16-byte line, for every row
     const uintptr_t a = reinterpret_cast<uintptr_t>(P.logits), c = reinterpret_cast<uintptr_t>(P.out);
     const bool vector = (a - c) % 16 == 0 && ((P.row_stride - P.out_stride) * esz) % 16 == 0;
-    P.after_copy = !in_place || P.mask;
-    if (P.after_copy) {
-        const int per = adjust_copy_entries(dtype);
-        const int most = P.V + (vector && (a % 16 || (P.row_stride * esz) % 16) ? 16 / esz - 1 : 0);  // with the entries before a row's start
-        P.pieces = (most + per - 1) / per;
-        // In place most rows have no mask as a rule, and a CTA that finds none has nothing to do: no more of them than fill the GPU.
-        P.turns = P.pieces;
-        while (in_place && P.turns > 1 && (long long)P.B * P.N * P.turns > 148 * 32) P.turns = (P.turns + 1) / 2;
-        const cudaError_t e = bf ? (in_place ? copy<DSSD_BF16, true>(P, vector, stream) : copy<DSSD_BF16, false>(P, vector, stream))
-                                 : (in_place ? copy<DSSD_F32, true>(P, vector, stream) : copy<DSSD_F32, false>(P, vector, stream));
-        if (e != cudaSuccess) return e;
+    const int per = adjust_copy_entries(dtype);
+    const int most = P.V + (vector && (a % 16 || (P.row_stride * esz) % 16) ? 16 / esz - 1 : 0);  // with the entries before a row's start
+    P.pieces = (most + per - 1) / per;
+    P.turns = P.pieces;
+    if (in_place) {
+        if (P.mask) {
+            // most rows have no mask as a rule, and a CTA that finds none has nothing to do: no more of them than fill the GPU a few times over
+            while (P.turns > 1 && (long long)P.B * P.N * P.turns > 148 * 64) P.turns = (P.turns + 1) / 2;
+            e = bf ? copy<DSSD_BF16, true>(P, vector, stream) : copy<DSSD_F32, true>(P, vector, stream);
+            if (e != cudaSuccess) return e;
+        }
+        P.gaps = (long long)P.slots * 3 / 4 < tokens;
+        const unsigned rows = (unsigned)((long long)P.B * P.N);
+        return bf ? launch_pdl(adjust_patch_kernel<DSSD_BF16>, rows, kThreads, stream, P) : launch_pdl(adjust_patch_kernel<DSSD_F32>, rows, kThreads, stream, P);
     }
-    // a slot and a third for each token that there may be
-    P.slots = 512;
-    while (P.slots < kMaxSlots && (long long)P.slots * 3 / 4 < (long long)P.L + P.N + P.K) P.slots *= 2;
-    // sequences alone on the GPU have their rows (or the ranges of a large table) shared out
-    P.shares = 1;
-    while (P.shares < 32 && (long long)P.B * P.shares < 2 * 148 && P.shares < P.N) P.shares *= 2;
-    return bf ? patch<DSSD_BF16>(P, stream) : patch<DSSD_F32>(P, stream);
+    return bf ? copy<DSSD_BF16, false>(P, vector, stream) : copy<DSSD_F32, false>(P, vector, stream);
 }
 
 }  // namespace dssd

@@ -511,7 +511,7 @@ Table table(const OnDevice &on, PyObject *o, int64_t B, const char *what)
 }
 
 // logits, history, prompt_len, history_len, draft_tokens, parents, repetition, presence, frequency, bias_tokens, bias_values,
-// mask, mask_row, out, stream
+// mask, mask_row, out, workspace, stream
 dssd_status adjust_logits(PyObject *const *a)
 {
     const Rows r = rows(a[0]);
@@ -552,9 +552,11 @@ dssd_status adjust_logits(PyObject *const *a)
         mask_row = values<const int32_t>(on, a[12], at::kInt, B * N, "mask_row must be an int32 [B, N] tensor");
     }
     uint32_t *fl = out_values<uint32_t>(on, a[13], "flags", at::kInt, B, true);
-    void *s = stream(a[14]);
+    const Space ws = space(a[14]);
+    require(tensor(a[14]).device() == on.device, "the workspace must be on the same device");
+    void *s = stream(a[15]);
     return call(lib.dssd_adjust_logits, r.data, r.dtype, r.stride, r.B, (int)N, r.V, tok, par, h.data, h.stride, h.n, pl, hl, rep, pre, fre,
-                bt, bv, K, mask, mask_rows, mask_row, o.data_ptr(), o_stride, fl, s);
+                bt, bv, K, mask, mask_rows, mask_row, o.data_ptr(), o_stride, fl, ws.data, ws.bytes, s);
 }
 
 dssd_dtype half_code(const at::Tensor &t)
@@ -724,7 +726,7 @@ PyMethodDef methods[] = {
     ENTRY(edge_emit_shard, 6),
     ENTRY(resample_shard_mass, 7),
     ENTRY(resample_shard_draw, 11),
-    ENTRY(adjust_logits, 15),
+    ENTRY(adjust_logits, 16),
     ENTRY(tree_attention, 12),
     ENTRY(tree_verify, 11),
     ENTRY(cache_append, 10),

@@ -39,13 +39,19 @@ dssd_status check_pages(const int32_t *table, int64_t table_stride, int max_page
 
 extern "C" {
 
+size_t dssd_adjust_logits_workspace_bytes(int B, int N, int V, int L, int K)
+{
+    if (check_tree(B, N, V) != DSSD_OK || V > DSSD_ADJUST_MAX_V || L < 0 || L >= 1 << 29 || K < 0 || K > 65535) return 0;
+    return dssd::adjust_workspace(B, N, V, L, K);
+}
+
 dssd_status dssd_adjust_logits(const void *logits, dssd_dtype dtype, int64_t row_stride, int B, int N, int V,
                                const int32_t *draft_tokens, const int32_t *parents, const int32_t *history,
                                int64_t history_stride, int L, const int32_t *prompt_len, const int32_t *history_len,
                                const float *repetition, const float *presence, const float *frequency,
                                const int32_t *bias_tokens, const float *bias_values, int K, const uint32_t *mask,
                                int mask_rows, const int32_t *mask_row, void *out, int64_t out_stride, uint32_t *flags,
-                               void *cuda_stream)
+                               void *workspace, size_t workspace_bytes, void *cuda_stream)
 {
     dssd::set_last_cuda_error(0);
     const dssd_status st = check_tree(B, N, V);
@@ -60,10 +66,11 @@ dssd_status dssd_adjust_logits(const void *logits, dssd_dtype dtype, int64_t row
     if (K > 0 && (!bias_tokens || !bias_values)) return DSSD_ERR_INVALID_ARG;
     if (mask_row && !mask && mask_rows > 0) return DSSD_ERR_INVALID_ARG;
     if (mask && !mask_row && (long long)mask_rows < (long long)B * N) return DSSD_ERR_INVALID_ARG;
-    if (K > 65535 || L >= 1 << 29) return DSSD_ERR_UNSUPPORTED;
+    if (K > 65535 || L >= 1 << 29 || V > DSSD_ADJUST_MAX_V) return DSSD_ERR_UNSUPPORTED;
     // CTAs of the copy
     const long long per = dssd::adjust_copy_entries((int)dtype);
-    if ((long long)B * N * ((V + per + 7) / per) > 0x7fffffff) return DSSD_ERR_UNSUPPORTED;
+    if ((long long)B * N * ((V + per + 7) / per) > 0x7fffffff || (long long)B * 16 > 0x7fffffff) return DSSD_ERR_UNSUPPORTED;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < dssd_adjust_logits_workspace_bytes(B, N, V, L, K)) return DSSD_ERR_WORKSPACE;
 
     dssd::AdjustParams P{};
     P.logits = logits;
@@ -85,7 +92,7 @@ dssd_status dssd_adjust_logits(const void *logits, dssd_dtype dtype, int64_t row
     P.mask_row = mask ? mask_row : nullptr;
     P.flags = flags;
     P.B = B, P.N = N, P.V = V, P.L = L, P.K = K, P.mask_rows = mask_rows;
-    return done(dssd::adjust_launch(P, (int)dtype, static_cast<cudaStream_t>(cuda_stream)));
+    return done(dssd::adjust_launch(P, (int)dtype, workspace, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 size_t dssd_tree_attention_workspace_bytes(int B, int N, int Hq, int Hkv, int D)

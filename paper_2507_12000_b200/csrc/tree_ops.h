@@ -25,12 +25,18 @@ struct AdjustParams {
     // geometry
     int pieces;  // of a row, each a turn of a CTA of the copy
     int turns;   // CTAs of the copy per row
-    int slots;   // of the patch's table, a power of two
-    int shares;  // CTAs of the patch per sequence
-    int after_copy;
+    int slots;   // of the table of tokens, a power of two
+    int shares;  // CTAs of the list per sequence
+    // workspace
+    uint4 *list;         // [B, list_size] entries, by buckets
+    int2 *buckets;       // [B, n_buckets] first entry and the one behind the last
+    long long list_size;
+    int n_buckets;
+    int gaps;            // buckets may not follow one another
 };
 int adjust_copy_entries(int dtype);  // of a row, by a CTA of the copy
-cudaError_t adjust_launch(AdjustParams &P, int dtype, cudaStream_t stream);
+size_t adjust_workspace(int B, int N, int V, int L, int K);
+cudaError_t adjust_launch(AdjustParams &P, int dtype, void *workspace, cudaStream_t stream);
 
 struct TreeVerifyParams {
     const void *logits;

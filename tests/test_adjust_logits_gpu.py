@@ -153,12 +153,13 @@ def test_mask_per_row_stream_and_graph(B):
     r = call(B, d, stream=s)
     check(r["logits"], d, ref, mag, live, np.zeros(ref.shape))
     out = {"logits": torch.zeros_like(d["logits"])}
+    ws = torch.full((B.dssd_adjust_logits_workspace_bytes(3, 4, 130, 50, 7),), 255, dtype=torch.uint8, device="cuda")
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):
         call_args = dict(d)
         B.dssd_adjust_logits(call_args["logits"], d["history"], d["prompt_len"], d["history_len"], draft_tokens=d["draft_tokens"], parents=d["parents"],
                              repetition=d["repetition"], presence=d["presence"], frequency=d["frequency"], bias_tokens=d["bias_tokens"],
-                             bias_values=d["bias_values"], mask=d["mask"], out=out)
+                             bias_values=d["bias_values"], mask=d["mask"], out=out, workspace=ws)
     d["logits"].mul_(0.5)
     d["history_len"].zero_()
     g.replay()

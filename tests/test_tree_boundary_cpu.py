@@ -25,7 +25,7 @@ def i64(*v):
 def adjust(B, /, **kw):
     a = dict(logits=P, dtype=0, row_stride=100, B=2, N=3, V=100, draft_tokens=P, parents=None, history=P, history_stride=9, L=9, prompt_len=P,
              history_len=P, repetition=None, presence=None, frequency=None, bias_tokens=P, bias_values=P, K=4, mask=P, mask_rows=2, mask_row=P,
-             out=2 * P, out_stride=100, flags=None, stream=None)
+             out=2 * P, out_stride=100, flags=None, workspace=P, bytes=1 << 40, stream=None)
     a.update(kw)
     return B.lib.dssd_adjust_logits(*a.values())
 
@@ -36,6 +36,7 @@ def adjust(B, /, **kw):
     (dict(prompt_len=None), 1), (dict(history_stride=8), 1), (dict(bias_tokens=None), 1), (dict(bias_values=None), 1), (dict(K=-1), 1),
     (dict(mask=None), 1), (dict(mask_row=None), 1), (dict(mask_rows=-1), 1), (dict(logits=P + 2), 1), (dict(dtype=2), 2), (dict(dtype=9), 2),
     (dict(N=129), 2), (dict(K=65536), 2), (dict(L=1 << 29, history_stride=1 << 29), 2), (dict(V=(1 << 30) + 1, row_stride=1 << 31, out_stride=1 << 31), 2),
+    (dict(V=(1 << 24) + 1, row_stride=1 << 31, out_stride=1 << 31), 2), (dict(workspace=None), 3), (dict(workspace=P + 8), 3), (dict(bytes=0), 3),
 ])
 def test_adjust_refuses(B, kw, status):
     assert adjust(B, **kw) == status
@@ -107,6 +108,13 @@ def test_workspace_sizes_never_decrease(B):
             if k == 4:
                 more[k] = 128
             assert f(*more) >= f(*a)
+    h = B.dssd_adjust_logits_workspace_bytes
+    assert h(0, 1, 10, 0, 0) == h(1, 129, 10, 0, 0) == h(1, 1, (1 << 24) + 1, 0, 0) == h(1, 1, 10, -1, 0) == h(1, 1, 10, 0, 65536) == 0
+    for a in ((1, 1, 1, 0, 0), (3, 17, 50272, 600, 32)):
+        for k in range(5):
+            more = list(a)
+            more[k] = 2 * more[k] + 1
+            assert h(*more) >= h(*a) > 0
     assert g(1, 2, 100) <= g(2, 2, 100) <= g(2, 128, 100) <= g(2, 128, 200000)
 
 
