@@ -6,7 +6,7 @@ the binding, which raises ImportError when the library has not been built: there
 """
 import importlib
 
-_SUBMODULES = ("binding", "build")
+_SUBMODULES = ("binding", "build", "tree")
 
 
 def __getattr__(name):
