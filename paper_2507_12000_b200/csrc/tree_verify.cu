@@ -611,11 +611,14 @@ cudaError_t tree_verify_launch(TreeVerifyParams &P, int dtype, void *workspace, 
 {
     (void)workspace;
     const int blocks = (P.V + kBlock - 1) / kBlock;
-    // Clusters of eight as long as every warp has a block: a sequence's passes follow one another, and the GPU holds many more sequences than
-    // eights of CTAs, so that long and short walks even out.  Sixteen where there are few sequences.
+    // A cluster of more CTAs makes a sequence's passes shorter, and lets fewer sequences walk at a time.  Two CTAs of this kernel fit an SM: as many
+    // to a sequence as leave room for all (us of 1 2 4 8 16 CTAs: B=8 V=32000 24.4 22.4 19.1 17.1 17.8; B=64 V=128256 150 94 64 69 102; B=160
+    // V=32000 113 77 70 95 200), but no CTA with more than 72 KB of a row (B=128 V=151936: 512 286 198 168 227; float32, B=86 V=86704: 132 with four, 109 with eight) and no warp without a block
+    // (B=160 V=8192: 48 40 51 83 176).  Sixteen where there are few sequences (B=2 V=50272: 33 27 21 17.5 16.6; B=16 V=128256: 94 56 37 28 31).
+    const int esz = dtype == DSSD_BF16 ? 2 : 4;
     unsigned ctas = 1;
-    while (ctas < 8 && blocks > kWarps * (int)ctas) ctas *= 2;
-    if (ctas == 8 && P.B <= 18 && blocks > kWarps * 8) ctas = 16;
+    while (ctas < 8 && blocks > kWarps * (int)ctas && ((long long)P.B * ctas * 2 <= 448 || (long long)P.V * esz > 72000ll * ctas)) ctas *= 2;
+    if (ctas == 8 && P.B <= 4 && blocks > kWarps * 8) ctas = 16;
     cudaError_t e = cudaErrorNotSupported;
     const bool shift = (P.V | P.row_stride) % 4 != 0 || reinterpret_cast<uintptr_t>(P.logits) % 16 != 0 || reinterpret_cast<uintptr_t>(P.draft_q) % 16 != 0;
     for (; e == cudaErrorNotSupported; ctas /= 2) {  // (a device that takes no clusters of sixteen)
