@@ -15,6 +15,7 @@ namespace dssd {
 namespace {
 
 constexpr int kLayers = 4;  // layers of a warp
+constexpr int kAtOnce = 4;  // pieces of K and of V that a lane has in flight
 
 // the page of appended position i, or -1 with the reason in *flags
 __device__ __forceinline__ int page_of(const AppendParams &P, long long b, int ctx, int i, int &place, unsigned &flags)
@@ -93,22 +94,25 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
     constexpr int kPer = sizeof(Word) / 2;  // elements of a piece
     const int per_head = P.D / kPer, pieces = P.Hkv * per_head;
     const int64_t from0 = b * P.new_b + node * P.new_n, to0 = page * P.cache_p + place * P.cache_t;
-    const int nl = min(kLayers, P.layers - l0);
-    for (int e = lane; e < pieces; e += 32) {
-        const int h = e / per_head, d = (e - h * per_head) * kPer;
-        const int64_t from = from0 + h * P.new_h + d, to = to0 + h * P.cache_h + d;
-        Word k[kLayers], v[kLayers];
+    const int items = min(kLayers, P.layers - l0) * pieces;
+    for (int x0 = lane; x0 < items; x0 += 32 * kAtOnce) {
+        Word k[kAtOnce], v[kAtOnce];
+        int64_t to[kAtOnce];
 #pragma unroll
-        for (int l = 0; l < kLayers; ++l) {
-            if (l >= nl) continue;
-            k[l] = piece<Word>(static_cast<const unsigned short *>(P.k_new) + from + (l0 + l) * P.new_l);
-            v[l] = piece<Word>(static_cast<const unsigned short *>(P.v_new) + from + (l0 + l) * P.new_l);
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int x = x0 + 32 * u;
+            if (x >= items) continue;
+            const int l = x / pieces, e = x - l * pieces, h = e / per_head, d = (e - h * per_head) * kPer;
+            const int64_t from = from0 + h * P.new_h + d + (l0 + l) * P.new_l;
+            to[u] = to0 + h * P.cache_h + d + (l0 + l) * P.cache_l;
+            k[u] = piece<Word>(static_cast<const unsigned short *>(P.k_new) + from);
+            v[u] = piece<Word>(static_cast<const unsigned short *>(P.v_new) + from);
         }
 #pragma unroll
-        for (int l = 0; l < kLayers; ++l) {
-            if (l >= nl) continue;
-            *reinterpret_cast<Word *>(static_cast<unsigned short *>(P.k_cache) + to + (l0 + l) * P.cache_l) = k[l];
-            *reinterpret_cast<Word *>(static_cast<unsigned short *>(P.v_cache) + to + (l0 + l) * P.cache_l) = v[l];
+        for (int u = 0; u < kAtOnce; ++u) {
+            if (x0 + 32 * u >= items) continue;
+            *reinterpret_cast<Word *>(static_cast<unsigned short *>(P.k_cache) + to[u]) = k[u];
+            *reinterpret_cast<Word *>(static_cast<unsigned short *>(P.v_cache) + to[u]) = v[u];
         }
     }
 }
