@@ -679,7 +679,8 @@ size_t dssd_tree_attention_workspace_bytes(int B, int N, int Hq, int Hkv, int D)
  * positions of its pages has no effect, NaN included.  A node sees no value of a node that is not its ancestor, unless
  * that value is infinite or NaN: then the rows of the whole sequence may be NaN.
  * D is a multiple of 8, at most 128; Hq a multiple of Hkv with Hq/Hkv <= 128; 1 <= N <= DSSD_TREE_MAX_NODES.  Every pointer to q, k, v and o
- * is 16-byte aligned and every stride a multiple of 8 elements (DSSD_ERR_UNSUPPORTED otherwise).
+ * is 16-byte aligned (DSSD_ERR_INVALID_ARG otherwise) and every stride a multiple of 8 elements, not 0 where there is more than one
+ * entry (DSSD_ERR_UNSUPPORTED otherwise).
  */
 dssd_status dssd_tree_attention(const void *q, const int64_t *q_strides, const void *k_new, const void *v_new,
                                 const int64_t *new_strides, const void *k_cache, const void *v_cache,
@@ -691,7 +692,7 @@ dssd_status dssd_tree_attention(const void *q, const int64_t *q_strides, const v
 
 #define DSSD_EDGE_FLAG_BAD_PARENT 8u /* dssd_tree_verify: see above */
 
-/* Bytes of scratch that dssd_tree_verify needs (0 if the sizes are invalid). */
+/* Bytes of scratch that dssd_tree_verify asks for (0 if the sizes are invalid; its present kernels use none). */
 size_t dssd_tree_verify_workspace_bytes(int B, int N, int V);
 
 /*
@@ -709,7 +710,8 @@ size_t dssd_tree_verify_workspace_bytes(int B, int N, int V);
  * For a chain this is dssd_dsd_verify.
  *
  * Only the rows of nodes on the accepted path are read, and draft rows of those with a rejection.
- * p, sums and the draw are evaluated in float64 (exponentials to 5e-11).  T is at most 1e30.  u == 1 never accepts; q <= 0 accepts iff the left over p > 0; a
+ * The verdict is that of exact arithmetic on the given values, to about 1e-10 of the distribution: what a float32 pass with a bound on its
+ * error cannot decide is decided in float64.  T, a float64 here, is at most 1e30.  u == 1 never accepts; q <= 0 accepts iff the left over p > 0; a
  * NaN q or an out-of-range token rejects.
  *
  * target_logits [B, N, V] float32 or bfloat16, row (b, j) at element (b*N+j)*row_stride
@@ -726,7 +728,7 @@ size_t dssd_tree_verify_workspace_bytes(int B, int N, int V);
  */
 dssd_status dssd_tree_verify(const void *target_logits, dssd_dtype dtype, int64_t row_stride, const float *draft_q,
                              const int32_t *draft_tokens, const int32_t *parents, const float *uniforms,
-                             const float *uniforms_rs, float temperature, int replacement, int B, int N, int V,
+                             const float *uniforms_rs, double temperature, int replacement, int B, int N, int V,
                              int32_t *accept_len, int32_t *path, int32_t *token, uint32_t *edge_flags,
                              uint32_t *rs_flags, void *workspace, size_t workspace_bytes, void *cuda_stream);
 

@@ -163,7 +163,7 @@ def _load(path: Optional[str] = None) -> ctypes.CDLL:
     L.dssd_tree_verify_workspace_bytes.restype = c.c_size_t
     L.dssd_tree_verify_workspace_bytes.argtypes = [i, i, i]
     L.dssd_tree_verify.restype = i
-    L.dssd_tree_verify.argtypes = [p, i, i64, p, p, p, p, p, c.c_float, i, i, i, i, p, p, p, p, p, p, c.c_size_t, p]
+    L.dssd_tree_verify.argtypes = [p, i, i64, p, p, p, p, p, c.c_double, i, i, i, i, p, p, p, p, p, p, c.c_size_t, p]
     L.dssd_cache_append.restype = i
     L.dssd_cache_append.argtypes = [p, p, p, p, p, p, i, p, i64, i, i, i, p, p, p, i, i, i, i, i, p, p, p]
     return L

@@ -627,7 +627,7 @@ dssd_status tree_verify(PyObject *const *a)
     const int32_t *par = values<const int32_t>(on, a[3], at::kInt, nodes, "parents must be an int32 [B, N-1] tensor");
     const float *u = values<const float>(on, a[4], at::kFloat, nodes, "uniforms must be a float32 [B, N-1] tensor");
     const float *ur = values<const float>(on, a[5], at::kFloat, B, "uniforms_rs must be a float32 [B] tensor");
-    const float T = (float)number(a[6]);
+    const double T = number(a[6]);
     const int with = PyObject_IsTrue(a[7]);
     int32_t *n = out_values<int32_t>(on, a[8], "accept_len", at::kInt, B), *path = out_values<int32_t>(on, a[8], "path", at::kInt, B * N);
     int32_t *token = out_values<int32_t>(on, a[8], "token", at::kInt, B);

@@ -125,6 +125,11 @@ dssd_status dssd_tree_attention(const void *q, const int64_t *q_strides, const v
         if (q_strides[i] < 0 || new_strides[i] < 0 || cache_strides[i] < 0 || o_strides[i] < 0) return DSSD_ERR_INVALID_ARG;
         if ((q_strides[i] | new_strides[i] | cache_strides[i] | o_strides[i]) % 8) return DSSD_ERR_UNSUPPORTED;
     }
+    // (a tiled copy takes no stride of nothing)
+    if ((B > 1 && (!q_strides[0] || !new_strides[0])) || (N > 1 && (!q_strides[1] || !new_strides[1])) || (Hq > 1 && !q_strides[2]) ||
+        (Hkv > 1 && (!new_strides[2] || (num_pages > 0 && !cache_strides[2]))) || (num_pages > 1 && !cache_strides[0]) ||
+        (num_pages > 0 && page_size > 1 && !cache_strides[1]))
+        return DSSD_ERR_UNSUPPORTED;
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < dssd_tree_attention_workspace_bytes(B, N, Hq, Hkv, D)) return DSSD_ERR_WORKSPACE;
 
     dssd::TreeAttentionParams P{};
@@ -149,12 +154,12 @@ dssd_status dssd_tree_attention(const void *q, const int64_t *q_strides, const v
 size_t dssd_tree_verify_workspace_bytes(int B, int N, int V)
 {
     if (check_tree(B, N, V) != DSSD_OK) return 0;
-    return dssd::tree_verify_workspace(B, N, V);
+    return 256;
 }
 
 dssd_status dssd_tree_verify(const void *target_logits, dssd_dtype dtype, int64_t row_stride, const float *draft_q,
                              const int32_t *draft_tokens, const int32_t *parents, const float *uniforms,
-                             const float *uniforms_rs, float temperature, int replacement, int B, int N, int V,
+                             const float *uniforms_rs, double temperature, int replacement, int B, int N, int V,
                              int32_t *accept_len, int32_t *path, int32_t *token, uint32_t *edge_flags,
                              uint32_t *rs_flags, void *workspace, size_t workspace_bytes, void *cuda_stream)
 {
@@ -164,9 +169,9 @@ dssd_status dssd_tree_verify(const void *target_logits, dssd_dtype dtype, int64_
     if (dtype != DSSD_F32 && dtype != DSSD_BF16) return DSSD_ERR_UNSUPPORTED;
     if (!target_logits || !uniforms_rs || !accept_len || !path || !token || row_stride < V) return DSSD_ERR_INVALID_ARG;
     if (N > 1 && (!draft_q || !draft_tokens || !uniforms)) return DSSD_ERR_INVALID_ARG;
-    if (!(temperature > 0.f) || !isfinite(temperature)) return DSSD_ERR_INVALID_ARG;
+    if (!(temperature > 0.0) || !isfinite(temperature)) return DSSD_ERR_INVALID_ARG;
     if (!aligned(target_logits, dtype == DSSD_BF16 ? 2 : 4) || !aligned(draft_q, 4)) return DSSD_ERR_INVALID_ARG;
-    if ((long long)B * 16 > 0x7fffffff || temperature > 1e30f) return DSSD_ERR_UNSUPPORTED;
+    if ((long long)B * 16 > 0x7fffffff || temperature > 1e30) return DSSD_ERR_UNSUPPORTED;
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < dssd_tree_verify_workspace_bytes(B, N, V)) return DSSD_ERR_WORKSPACE;
 
     dssd::TreeVerifyParams P{};
@@ -177,7 +182,7 @@ dssd_status dssd_tree_verify(const void *target_logits, dssd_dtype dtype, int64_
     P.parents = parents;
     P.uniforms = uniforms;
     P.uniforms_rs = uniforms_rs;
-    P.c1 = 1.4426950408889634074 / (double)temperature;
+    P.c1 = 1.4426950408889634074 / temperature;
     P.replacement = replacement != 0;
     P.B = B, P.N = N, P.V = V;
     P.accept_len = accept_len;
@@ -185,7 +190,7 @@ dssd_status dssd_tree_verify(const void *target_logits, dssd_dtype dtype, int64_
     P.token = token;
     P.edge_flags = edge_flags;
     P.rs_flags = rs_flags;
-    return done(dssd::tree_verify_launch(P, (int)dtype, workspace, static_cast<cudaStream_t>(cuda_stream)));
+    return done(dssd::tree_verify_launch(P, (int)dtype, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 dssd_status dssd_cache_append(const void *k_new, const void *v_new, const int64_t *new_strides, void *k_cache,

@@ -44,15 +44,15 @@ struct TreeVerifyParams {
     const float *draft_q;
     const int32_t *draft_tokens, *parents;
     const float *uniforms, *uniforms_rs;
-    double c1;  // log2(e) / T
+    double c1;         // log2(e) / T
+    double sum_error;  // of a float32 pass
     int replacement, B, N, V;
     int32_t *accept_len, *path, *token;
     uint32_t *edge_flags, *rs_flags;
     int slice;  // entries of the vocabulary per CTA of the sequence's cluster
     int chunk;  // entries of a warp at a time
 };
-size_t tree_verify_workspace(int B, int N, int V);
-cudaError_t tree_verify_launch(TreeVerifyParams &P, int dtype, void *workspace, cudaStream_t stream);
+cudaError_t tree_verify_launch(TreeVerifyParams &P, int dtype, cudaStream_t stream);
 
 struct AppendParams {
     const void *k_new, *v_new;

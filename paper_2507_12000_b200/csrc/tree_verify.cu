@@ -17,6 +17,8 @@
 // entry: 2^x by a table of 16 entries, each in banks of its own, and a polynomial).  With everything in float64 the verdicts of B=128 N=12 V=151936 took 232 us.
 //
 // Bound by the latency of a chain of dependent reductions for few sequences, by the visited rows for many.
+#include <math.h>
+
 #include "launch.h"
 #include "quads.cuh"
 #include "tree.cuh"
@@ -41,10 +43,10 @@ struct VerifySmem {
     unsigned long long again[1];  // the draw was not certain
 };
 
-// Bounds of the errors of a float32 pass, relative to the whole distribution: a sum of p over any entries, divided by the row's.  Per term:
-// ex2 2^-22; the rounding of x = l c1 - ref, 2^-25 |x|, of which p weighs 17 bits at the most for 10^5 entries; sixteen float32 additions in a tree of
-// four.  Twice that, for the row's sum.  (c1 is rounded to float32 on this path: p is that of a temperature 3e-8 off, 1e-7 of p.)
-constexpr double kSumError = 1.5e-6;
+// Bounds of the errors of a float32 pass, relative to the whole distribution, of a sum of p over any entries.  In numerator and row's sum alike, per term: ex2,
+// 2^-22; the rounding of x = l c1 - ref, ln(2) 2^-24 |x|, where sum p |x| is at most the logarithm of the number of entries; the rounding of c1, half of that at the
+// most between entries; six levels of float32 additions of 2^-24.
+__host__ inline double sum_error(int V) { return 2.0 * (2.4e-7 + 4.2e-8 * (1.5 * log2((double)V + 1.0)) + 6.0 * 6.0e-8); }
 constexpr double kProductError = 2.5e-7;  // of a q in the residual, for each unit of a
 
 __device__ __forceinline__ double as_double(int hi, int lo) { return __hiloint2double(hi, lo); }
@@ -328,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
         inv = 1.0 / sum;
         a = 0.0, m = 1.0, c = 1.0, gone = 0.0;
         a_error = m_error = 0.0;
-        const double slack = fine ? 0.0 : kSumError, C = fine ? P.c1 : (double)c1;
+        const double slack = fine ? 0.0 : P.sum_error, C = fine ? P.c1 : (double)c1;
         bool taken = false;
         while (j > 0) {
             if (!next.ok) eflags |= DSSD_EDGE_FLAG_BAD_TOKEN;
@@ -475,7 +477,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
         if (invalid) rflags |= DSSD_RS_FLAG_INVALID;
         if (invalid) owner = 0;
         // the uniform's place and the steps of the distribution have to be further apart than this
-        const double margin = fine ? -1.0 : 2.0 * sum * (a > 0.0 ? m_error : kSumError);
+        const double margin = fine ? -1.0 : 2.0 * sum * (a > 0.0 ? m_error : P.sum_error);
         if (me == (unsigned)owner && warp == 0) {
             int token = -1;
             bool sure = true;
@@ -601,15 +603,9 @@ cudaError_t launch_as(const TreeVerifyParams &P, unsigned ctas, cudaStream_t str
 
 }  // namespace
 
-size_t tree_verify_workspace(int B, int N, int V)
+cudaError_t tree_verify_launch(TreeVerifyParams &P, int dtype, cudaStream_t stream)
 {
-    (void)V;
-    return (((size_t)B * (size_t)N * 16) + 255) & ~(size_t)255;
-}
-
-cudaError_t tree_verify_launch(TreeVerifyParams &P, int dtype, void *workspace, cudaStream_t stream)
-{
-    (void)workspace;
+    P.sum_error = sum_error(P.V);
     const int blocks = (P.V + kBlock - 1) / kBlock;
     // A cluster of more CTAs makes a sequence's passes shorter, and lets fewer sequences walk at a time.  Two CTAs of this kernel fit an SM: as many
     // to a sequence as leave room for all (us of 1 2 4 8 16 CTAs: B=8 V=32000 24.4 22.4 19.1 17.1 17.8; B=64 V=128256 150 94 64 69 102; B=160

@@ -117,6 +117,26 @@ def test_garbage_in_unused_places(B):
         assert torch.equal(out["o"][~dead], ref[~dead]) and (out["o"][dead] == 2.5).all() and (out["flags"] == 0).all()
 
 
+def test_without_a_cache(B):
+    """No pages at all, a table without columns, a table of pages that do not exist: the nodes see each other."""
+    d = make(21, 3, 7, 4, 2, 64, 16, [0, 0, 0], torch.bfloat16)
+    ref = call(B, d)["o"]
+    check(ref, d)
+    none = torch.empty(0, 16, 2, 64, dtype=torch.bfloat16, device="cuda")
+    e = dict(d, k_cache=none, v_cache=none, block_table=torch.empty(3, 0, dtype=torch.int32, device="cuda"))
+    assert torch.equal(call(B, e)["o"], ref)
+    assert torch.equal(call(B, dict(e, block_table=torch.full((3, 2), 5, dtype=torch.int32, device="cuda")))["o"], ref)
+
+
+def test_many_sequences_and_pieces_that_begin_everywhere(B):
+    """More items than CTAs, and lengths that put the pieces' ends on, before and behind the items' ends."""
+    d = make(22, 150, 2, 4, 4, 64, 64, [(37 * i) % 513 for i in range(150)], torch.float16)
+    r = call(B, d, want_lse=True)
+    check(r["o"], d, lse=r["lse"])
+    d = make(23, 37, 3, 2, 2, 128, 32, [128] * 37, torch.bfloat16)
+    check(call(B, d)["o"], d)
+
+
 def test_views(B):
     """Queries, keys and values of one projection, a cache with the heads before the positions, an output inside a larger one."""
     d = make(7, 2, 6, 8, 2, 64, 16, [100, 40], torch.float16)

@@ -56,6 +56,7 @@ def attend(B, /, **kw):
     (dict(page_size=0), 1), (dict(table_stride=7), 1), (dict(num_pages=-1), 1), (dict(max_pages=-1), 1), (dict(scale=0.0), 1),
     (dict(scale=float("nan")), 1), (dict(q=P + 8), 1), (dict(v_cache=P + 2), 1), (dict(o=P + 4), 1), (dict(q_strides=i64(1024, -512, 128)), 1),
     (dict(dtype=0), 2), (dict(N=129), 2), (dict(D=12), 2), (dict(D=136), 2), (dict(Hq=258, Hkv=2), 2), (dict(new_strides=i64(1024, 256, 130)), 2),
+    (dict(q_strides=i64(0, 512, 128)), 2), (dict(new_strides=i64(1024, 256, 0)), 2), (dict(cache_strides=i64(0, 256, 128)), 2),
     (dict(max_pages=1 << 20, table_stride=1 << 20, page_size=1 << 12), 2), (dict(workspace=None), 3), (dict(workspace=P + 16), 3), (dict(bytes=0), 3),
 ])
 def test_attention_refuses(B, kw, status):

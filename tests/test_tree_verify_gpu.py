@@ -147,6 +147,29 @@ def test_every_sibling_refused_without_replacement(B):
     assert r["accept_len"][0] in (0, 1)
 
 
+def test_decisions_on_the_edge(B):
+    """Uniforms put within float32's errors of a test's or a step's edge, from both sides: the verdict is the exact one."""
+    rng = np.random.default_rng(31)
+    nb, V, T = 400, 3001, 0.9
+    d = R.verify_inputs(rng, nb, 2, V, torch.float32, T=T, sigma=1.2, parents=None)
+    x = R.f64(d["target_logits"])[:, 0] / T
+    p = np.exp(x - x.max(axis=1, keepdims=True))
+    p /= p.sum(axis=1, keepdims=True)
+    q = R.f64(d["draft_q"])[:, 0]
+    tok = d["draft_tokens"][:, 0].cpu().numpy()
+    ratio = p[np.arange(nb), tok] / q[np.arange(nb), tok]
+    u = np.minimum(ratio, 0.9).astype(np.float32)
+    u = np.where(np.arange(nb) % 2 == 0, np.nextafter(u, np.float32(0)), np.nextafter(u, np.float32(1)))
+    rest = np.maximum(p - q, 0)
+    cdf = np.cumsum(rest, axis=1)
+    step = rng.integers(0, V, nb)
+    ur = (cdf[np.arange(nb), step] / cdf[:, -1]).astype(np.float32)
+    ur = np.clip(np.where(np.arange(nb) % 3 == 0, np.nextafter(ur, np.float32(0)), ur), 0, np.float32(1 - 2 ** -24))
+    d["uniforms"] = torch.from_numpy(u[:, None].copy()).cuda()
+    d["uniforms_rs"] = torch.from_numpy(ur).cuda()
+    same(call(B, d, T, True), R.verify(d, T, True))
+
+
 def test_strided_rows_other_stream_graph_and_garbage(B):
     rng = np.random.default_rng(8)
     d = R.verify_inputs(rng, 6, 7, 3001, torch.bfloat16)
