@@ -34,7 +34,8 @@ namespace {
 
 constexpr int kTile = 128;      // keys of a tile, rows of a tile
 constexpr int kMaxCtas = 148;   // pieces of the line
-constexpr int kMinTiles = 2;    // tiles to a piece at least
+// tiles to a piece at least (us with 1, 2 and 4: B=1 N=1 ctx 2047 16.4 18.0 20.1; B=20 N=9 ctx 29 17.1 11.6 17.7; B=2 N=11 ctx 4760 18.8 16.6 18.1)
+constexpr int kMinTiles = 2;
 constexpr int kAttend = 384;     // threads: copies, products and an idle warp; the two groups of the softmax
 
 struct Geometry {
@@ -154,7 +155,7 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi)
 
 template <int DP, int kMT>
 struct Smem {
-    static constexpr int kStages = DP == 64 ? (kMT == 1 ? 5 : 5) : (kMT == 1 ? 3 : 2);
+    static constexpr int kStages = DP == 64 ? 5 : kMT == 1 ? 3 : 2;
     static constexpr int kChunk = kTile * 128;             // 64 columns of a tile
     static constexpr int kOperand = kTile * DP * 2;
     static constexpr int kQ = 0, kKV = kMT * kOperand;     // then K and V of the stages in turn
