@@ -55,7 +55,7 @@ const char *dssd_status_string(int status)
     }
 }
 
-int dssd_version(void) { return 100; }
+int dssd_version(void) { return 200; }
 
 int dssd_last_cuda_error(void) { return t_last_cuda_error; }
 
