@@ -171,7 +171,8 @@ dssd_status dssd_tree_verify(const void *target_logits, dssd_dtype dtype, int64_
     if (N > 1 && (!draft_q || !draft_tokens || !uniforms)) return DSSD_ERR_INVALID_ARG;
     if (!(temperature > 0.0) || !isfinite(temperature)) return DSSD_ERR_INVALID_ARG;
     if (!aligned(target_logits, dtype == DSSD_BF16 ? 2 : 4) || !aligned(draft_q, 4)) return DSSD_ERR_INVALID_ARG;
-    if ((long long)B * 16 > 0x7fffffff || temperature > 1e30) return DSSD_ERR_UNSUPPORTED;
+    // (beyond these log2(e) / T is no number of float32, or masked entries come near the others)
+    if ((long long)B * 16 > 0x7fffffff || temperature > 1e30 || temperature < 1e-30) return DSSD_ERR_UNSUPPORTED;
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < dssd_tree_verify_workspace_bytes(B, N, V)) return DSSD_ERR_WORKSPACE;
 
     dssd::TreeVerifyParams P{};
