@@ -51,14 +51,17 @@ constexpr double kProductError = 2.5e-7;  // of a q in the residual, for each un
 
 __device__ __forceinline__ double as_double(int hi, int lo) { return __hiloint2double(hi, lo); }
 
-// A logit as float64 by its bits (a conversion instruction has a quarter of the throughput of a product).  Zeros become 2^-127; infinities and NaN
-// become numbers of 2^128 and more.
-template <int DT>
-__device__ __forceinline__ double widen(uint32_t w)  // the bits of a float32
+// A float32 as float64 by its bits, 2^896 times too small (a conversion instruction has a quarter of the throughput of a product): exact for zeros and
+// subnormal numbers too.  Infinities and NaN become numbers of that size times 2^128 and more.
+__device__ __forceinline__ double shrunk(uint32_t w)
 {
-    const int hi = (int)(((w & 0x7fffffffu) >> 3) + 0x38000000u | (w & 0x80000000u));
-    return as_double(hi, DT == DSSD_BF16 ? 0 : (int)(w << 29));
+    return as_double((int)((w & 0x7fffffffu) >> 3 | (w & 0x80000000u)), (int)(w << 29));
 }
+constexpr double kGrow = 0x1p896, kGrowA = 0x1p803, kGrowS = 0x1p93;  // (of which the product is the first)
+
+// p - a q in units of the row's sum: a and s come with their part of the factor.  a q comes first, so that a large a meets what is small; a is below 2^156
+// and the sum below 2^931, so that neither part overflows.
+__device__ __forceinline__ double residual(double p, uint32_t q, double a, double s) { return __fma_rn(-s, shrunk(q) * a, p); }
 
 // 2^x = 2^(k / 16) 2^r, |r| <= 1/32; the polynomial is the exponential series to the fourth power (relative error below 5e-11).
 // 0 below 2^-1000, infinity above 2^1000.
@@ -204,6 +207,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
     double a_error = 0.0, m_error = 0.0;
     bool alive = true, fine = false;
     const float c1 = (float)P.c1;
+    const double c1_grown = P.c1 * kGrow;
     const char *row;
     const float *qrow;
     // what a test needs, asked for before the pass that comes before it
@@ -290,7 +294,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 const uint32_t x = E::bits(q, i);
-                                part += exp2_64(__fma_rn(widen<DT>(x), P.c1, -ref), S.table);
+                                part += exp2_64(__fma_rn(shrunk(x), c1_grown, -ref), S.table);
                                 if (is_nan(x)) part = __longlong_as_double(0x7ff8000000000000ll);
                             }
                         }
@@ -330,13 +334,13 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
         inv = 1.0 / sum;
         a = 0.0, m = 1.0, c = 1.0, gone = 0.0;
         a_error = m_error = 0.0;
-        const double slack = fine ? 0.0 : P.sum_error, C = fine ? P.c1 : (double)c1;
+        const double slack = fine ? 0.0 : P.sum_error, C = (fine ? P.c1 : (double)c1) * kGrow;
         bool taken = false;
         while (j > 0) {
             if (!next.ok) eflags |= DSSD_EDGE_FLAG_BAD_TOKEN;
             if (next.ok && alive) {
                 const double qx = (double)next.q, u = (double)next.u;
-                const double px = exp2_64(__fma_rn(widen<DT>(next.l), C, -ref), S.table) * inv;
+                const double px = exp2_64(__fma_rn(shrunk(next.l), C, -ref), S.table) * inv;
                 const double left = fmax(px - a * qx, 0.0), want = u * (c * m) * qx;
                 taken = u < 1.0 && (qx <= 0.0 ? left > 0.0 : want < left);
                 // (a NaN q rejects, whatever the errors)
@@ -351,7 +355,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
             a_error += c * m_error;
             if (!P.replacement) {
                 if (next.ok && next.q > 0.f) gone += (double)next.q;
-                c = 1.0 / fmax(1.0 - gone, 1e-300);  // (nothing left of q: p where q has no mass)
+                c = gone < 1.0 ? 1.0 / (1.0 - gone) : 0.0;  // (nothing left of q: nothing more is subtracted)
             }
             if (!fine && alive && !(a < 1e6)) {
                 certain = false;
@@ -403,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
                 }
                 m = (kept ? total : part) * as_double((1023 + e) << 20, 0);
             } else {
-                const double aS = a * sum;
+                const double aG = a * kGrowA, sG = sum * kGrowS;
                 while (w.more()) {
 #pragma unroll 1
                     for (int half = 0; half < kBlock; half += kBlock / 2) {
@@ -417,9 +421,9 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
                             const uint4 q = R.at(u);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                const double p = exp2_64(__fma_rn(widen<DT>(E::bits(l, i)), P.c1, -ref), S.table);
+                                const double p = exp2_64(__fma_rn(shrunk(E::bits(l, i)), c1_grown, -ref), S.table);
                                 const uint32_t qb = i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w;
-                                const double d = __fma_rn(-aS, widen<DSSD_F32>(qb), p);  // (a q of zero is 2^-127: below any p)
+                                const double d = residual(p, qb, aG, sG);
                                 part += d > 0.0 ? d : 0.0;
                             }
                         }
@@ -460,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
         // What the exchange after the last pass left: the CTAs' sums, in units of the row's.  The chunks' sums of a float32 pass over p - a q are
         // in units of a power of two below that.
         const double unit = !fine && a > 0.0 ? as_double((1023 + exponent(sum)) << 20, 0) : 1.0;
-        const double aS = a * sum, total = a > 0.0 ? m * sum : sum, target = u_draw * total;
+        const double aG = a * kGrowA, sG = sum * kGrowS, total = a > 0.0 ? m * sum : sum, target = u_draw * total;
         const double *const parts = S.part[turn ^ 1];
         int owner = -1, last = 0;  // last: the last CTA with mass
         double run = 0.0, before = 0.0;
@@ -521,8 +525,8 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
                     for (int i = 0; i < 16; ++i) q16[i] = a > 0.0 && v + i < e ? ld_row_u32(qrow + v + i) : 0u;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const double p = exp2_64(__fma_rn(widen<DT>(l16[i]), C, -ref), S.table);
-                        const double d = a > 0.0 ? __fma_rn(-aS, widen<DSSD_F32>(q16[i]), p) : p;
+                        const double p = exp2_64(__fma_rn(shrunk(l16[i]), C, -ref), S.table);
+                        const double d = a > 0.0 ? residual(p, q16[i], aG, sG) : p;
                         w[i] = d > 0.0 ? d : 0.0;
                     }
 #pragma unroll
