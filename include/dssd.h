@@ -703,8 +703,9 @@ size_t dssd_tree_verify_workspace_bytes(int B, int N, int V);
  *   u_j * c * m * q(x_j) < max(0, p(x_j) - a * q(x_j)).
  * After a rejection the residual distribution is max(0, p - a q) / m with
  *   a <- a + c * m,  m <- sum_v max(0, p_v - a q_v),
- * and, where siblings are drawn without replacement (replacement == 0), c <- 1 / (1 - sum of the q of the rejected siblings):
- * p_{r+1} = norm(max(0, p_r - q_r)) for every r, in closed form.  An accepted child becomes the node; where no
+ * and, where siblings are drawn without replacement (replacement == 0), c <- 1 / (sum of q over the tokens that are not among the rejected
+ * siblings), or 0 where that is 0 (nothing is subtracted any more): p_{r+1} = norm(max(0, p_r - q_r)) for every r, in closed form, where q_r is
+ * what is left of q, scaled to a sum of 1.  An accepted child becomes the node; where no
  * child is accepted (or there is none) the token is drawn from max(0, p - a q) with u', by inverse CDF
  * in index order as dssd_device_resample does (the fallback to p included).  Every emitted token follows the target distribution.
  * For a chain this is dssd_dsd_verify.

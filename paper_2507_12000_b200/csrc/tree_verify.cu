@@ -3,8 +3,9 @@
 // After r rejections at a node the residual distribution is max(0, p - a q) / m with two numbers a and m:
 //   max(0, max(0, p - a q) / m - c q) = max(0, p - (a + m c) q) / m,
 // (inside the outer maximum nothing changes where p - a q < 0, since q >= 0), so a rejection is one sum over the two rows
-// as they lie in memory and no row is ever written.  Drawing siblings without replacement only scales q by c between them:
-// a rejected token x has p(x) - a q(x) <= 0 from then on, so that its removal from q is not seen.
+// as they lie in memory and no row is ever written.  Drawing siblings without replacement only scales q by c between them, one divided by the sum of what
+// is left of q: a rejected token x has p(x) - a q(x) <= 0 from then on, so that its removal from q is not seen.  That sum is taken over the tokens that are
+// left, in the pass that reads q anyway, whenever another sibling follows: one minus the rejected ones has no digits left after a sibling that the draft was sure of.
 //
 // Every CTA of the cluster holds a slice of the vocabulary and the same scalars; sums meet through
 // distributed shared memory and are added in rank order by everybody, so that all CTAs take the same way.  A node costs one pass over its logits
@@ -34,8 +35,8 @@ constexpr int kBlock = 512;       // entries that a warp loads at once
 
 struct VerifySmem {
     double table[16];
-    double part[2][kMaxCluster];  // what the CTAs of the cluster exchange, in turns
-    double warp[2][kWarps];
+    double part[2][kMaxCluster], part2[2][kMaxCluster];  // what the CTAs of the cluster exchange, in turns
+    double warp[2][kWarps], warp2[2][kWarps];
     double chunk[kMaxChunks];
     int token[kMaxNodes];
     short parent[kMaxNodes], child[kMaxNodes], sibling[kMaxNodes];
@@ -48,6 +49,7 @@ struct VerifySmem {
 // most between entries; six levels of float32 additions of 2^-24.
 __host__ inline double sum_error(int V) { return 2.0 * (2.4e-7 + 4.2e-8 * (1.5 * log2((double)V + 1.0)) + 6.0 * 6.0e-8); }
 constexpr double kProductError = 2.5e-7;  // of a q in the residual, for each unit of a
+constexpr double kRestError = 4e-7;       // of what is left of q, relative: six levels of float32 additions
 
 __device__ __forceinline__ double as_double(int hi, int lo) { return __hiloint2double(hi, lo); }
 
@@ -82,23 +84,38 @@ __device__ __forceinline__ double exp2_64(double x, const double *table)
     return as_double(yh, far ? 0 : __double2loint(y));
 }
 
-// x of all threads, warps in order and CTAs in rank order; the same in every thread
-__device__ __forceinline__ double cluster_sum(VerifySmem &S, double x, unsigned ctas, int &turn)
+// x of all threads, and y where it is wanted: warps in order and CTAs in rank order; the same in every thread
+template <bool kBoth>
+__device__ __forceinline__ double cluster_sum(VerifySmem &S, double x, double &y, unsigned ctas, int &turn)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     x = warp_sum(x);
-    if (lane == 0) S.warp[turn][warp] = x;
+    if (kBoth) y = warp_sum(y);
+    if (lane == 0) {
+        S.warp[turn][warp] = x;
+        if (kBoth) S.warp2[turn][warp] = y;
+    }
     __syncthreads();
-    double s = 0.0;
+    double s = 0.0, s2 = 0.0;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) s += S.warp[turn][w];
+    for (int w = 0; w < kWarps; ++w) {
+        s += S.warp[turn][w];
+        if (kBoth) s2 += S.warp2[turn][w];
+    }
     if (ctas > 1) {
-        if (threadIdx.x < ctas) cluster_store(&S.part[turn][cluster_rank()], threadIdx.x, s);
+        if (threadIdx.x < ctas) {
+            cluster_store(&S.part[turn][cluster_rank()], threadIdx.x, s);
+            if (kBoth) cluster_store(&S.part2[turn][cluster_rank()], threadIdx.x, s2);
+        }
         cluster_arrive();
         cluster_wait();
-        s = 0.0;
-        for (unsigned c = 0; c < ctas; ++c) s += S.part[turn][c];
+        s = s2 = 0.0;
+        for (unsigned c = 0; c < ctas; ++c) {
+            s += S.part[turn][c];
+            if (kBoth) s2 += S.part2[turn][c];
+        }
     }
+    if (kBoth) y = s2;
     turn ^= 1;  // (a thread that is here again has seen every other thread's arrival at the exchange between)
     return s;
 }
@@ -165,8 +182,8 @@ __device__ __forceinline__ void prefetch_l2(const void *p, int bytes)
 
 __device__ __forceinline__ int exponent(double x) { return ((__double2hiint(x) >> 20) & 0x7ff) - 1023; }
 
-// kShift: rows may begin off the boundaries of four entries
-template <int DT, bool kShift>
+// kShift: rows may begin off the boundaries of four entries.  kWithout: siblings were drawn without replacement.
+template <int DT, bool kShift, bool kWithout>
 __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_constant__ TreeVerifyParams P)
 {
     typedef Logits<DT> E;
@@ -203,8 +220,9 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
     unsigned eflags = S.bad ? DSSD_EDGE_FLAG_BAD_PARENT : 0u, rflags = 0;
 
     int node = 0, length = 0;
-    double a = 0.0, m = 1.0, c = 1.0, gone = 0.0, ref = 0.0, sum = 1.0, inv = 1.0;
-    double a_error = 0.0, m_error = 0.0;
+    double a = 0.0, m = 1.0, c = 1.0, ref = 0.0, sum = 1.0, inv = 1.0;
+    double a_error = 0.0, m_error = 0.0, c_error = 0.0;
+    int refused = 0, mine = -1;  // siblings so far; the one of this lane's number
     bool alive = true, fine = false;
     const float c1 = (float)P.c1;
     const double c1_grown = P.c1 * kGrow;
@@ -303,7 +321,8 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
                     close(kept, w.next(), k, part, total);
                 }
             }
-            sum = cluster_sum(S, kept ? total : part, ctas, turn);
+            double none = 0.0;
+            sum = cluster_sum<false>(S, kept ? total : part, none, ctas, turn);
         }
         alive = sum == sum;
         if (alive && !(sum > 1e-280 && sum < 1e280)) {
@@ -332,10 +351,12 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
         }
         if (!alive) eflags |= DSSD_EDGE_FLAG_NONFINITE;
         inv = 1.0 / sum;
-        a = 0.0, m = 1.0, c = 1.0, gone = 0.0;
-        a_error = m_error = 0.0;
+        a = 0.0, m = 1.0, c = 1.0;
+        a_error = m_error = c_error = 0.0;
+        refused = 0, mine = -1;
         const double slack = fine ? 0.0 : P.sum_error, C = (fine ? P.c1 : (double)c1) * kGrow;
         bool taken = false;
+        auto more_error = [&] { return kWithout ? c * (m_error + m * c_error) : m_error; };  // of c m
         while (j > 0) {
             if (!next.ok) eflags |= DSSD_EDGE_FLAG_BAD_TOKEN;
             if (next.ok && alive) {
@@ -344,7 +365,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
                 const double left = fmax(px - a * qx, 0.0), want = u * (c * m) * qx;
                 taken = u < 1.0 && (qx <= 0.0 ? left > 0.0 : want < left);
                 // (a NaN q rejects, whatever the errors)
-                if (!fine && u < 1.0 && qx > 0.0 && !(fabs(px - a * qx - want) > px * slack + qx * (a_error + u * c * m_error))) {
+                if (!fine && u < 1.0 && qx > 0.0 && !(fabs(px - a * qx - want) > px * slack + qx * (a_error + u * more_error()))) {
                     certain = false;
                     break;
                 }
@@ -352,11 +373,8 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
             }
             // rejected: what is left of p
             a += c * m;
-            a_error += c * m_error;
-            if (!P.replacement) {
-                if (next.ok && next.q > 0.f) gone += (double)next.q;
-                c = gone < 1.0 ? 1.0 / (1.0 - gone) : 0.0;  // (nothing left of q: nothing more is subtracted)
-            }
+            a_error += more_error();
+            if (kWithout && next.ok && refused++ == lane) mine = S.token[j];
             if (!fine && alive && !(a < 1e6)) {
                 certain = false;
                 break;
@@ -366,8 +384,24 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
             kept = j == 0;
             m = 0.0;
             if (!alive) continue;
-            // the sum of max(0, p - a q): in float64 in units of the row's sum, in float32 in units of the power of two below it
-            double part = 0.0, total = 0.0;
+            // the sum of max(0, p - a q): in float64 in units of the row's sum, in float32 in units of the power of two below it; and of q over the tokens
+            // that were not refused
+            double part = 0.0, total = 0.0, rest = 0.0;
+            const bool follows = kWithout && j > 0;
+            // which of this lane's entries, in blocks of 128 from `from` on, are refused tokens: bit 4 u + i for entry i of its quad of block u
+            auto refused_in = [&](int from, int count) {
+                uint32_t bits = 0;
+                auto add = [&](int x) {
+                    const int at = x - from;
+                    if (at >= 0 && at < count && (at >> 2 & 31) == lane) bits |= 1u << (at >> 7) * 4 + (at & 3);
+                };
+                if (refused > 32)
+                    for (int k = S.child[node]; k != j; k = S.sibling[k]) add(S.token[k]);
+                else
+                    for (unsigned some = __ballot_sync(0xffffffffu, mine >= from && mine < from + count); some; some &= some - 1)
+                        add(__shfl_sync(0xffffffffu, mine, __ffs(some) - 1));
+                return bits;
+            };
             Walk w(slice, warp);
             if (!fine) {
                 const int e = exponent(sum);
@@ -384,6 +418,27 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
                     uint4 q[4];
 #pragma unroll
                     for (int u = 0; u < 4; ++u) l[u] = N.at(u), q[u] = NQ.at(u);
+                    if (follows) {
+                        const uint32_t gone = refused_in(w.at, kBlock);
+                        f32x2 s2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+                        if (__any_sync(0xffffffffu, gone)) {
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) {
+                                const uint32_t g = gone >> 4 * u;
+                                s2[0] = add2(s2[0], pack2(g & 1u ? 0.f : __uint_as_float(q[u].x), g & 2u ? 0.f : __uint_as_float(q[u].y)));
+                                s2[1] = add2(s2[1], pack2(g & 4u ? 0.f : __uint_as_float(q[u].z), g & 8u ? 0.f : __uint_as_float(q[u].w)));
+                            }
+                        } else {
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) {
+                                s2[0] = add2(s2[0], pack2(__uint_as_float(q[u].x), __uint_as_float(q[u].y)));
+                                s2[1] = add2(s2[1], pack2(__uint_as_float(q[u].z), __uint_as_float(q[u].w)));
+                            }
+                        }
+                        float x, y;
+                        unpack2(add2(s2[0], s2[1]), x, y);
+                        rest += (double)(x + y);
+                    }
                     const int k = w.k;
                     const bool ends = w.next();
                     if (w.more()) {
@@ -415,6 +470,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
                         WarpQuads<Quads32, 2, kShift> R;
                         L.load(row, P.V, w.at + half, E::kFill);
                         R.load(reinterpret_cast<const char *>(qrow), P.V, w.at + half, 0u);
+                        const uint32_t gone = follows ? refused_in(w.at + half, kBlock / 2) : 0u;
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
                             const typename E::Q::Raw l = L.at(u);
@@ -425,6 +481,8 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
                                 const uint32_t qb = i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w;
                                 const double d = residual(p, qb, aG, sG);
                                 part += d > 0.0 ? d : 0.0;
+                                // (positive and finite)
+                                if (follows && qb - 1u < 0x7f7fffffu && !(gone >> (4 * u + i) & 1u)) rest += shrunk(qb);
                             }
                         }
                     }
@@ -432,8 +490,17 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
                     close(kept, w.next(), k, part, total);
                 }
                 m = kept ? total : part;
+                rest *= kGrow;
             }
-            m = cluster_sum(S, m, ctas, turn) * inv;
+            m = cluster_sum<kWithout>(S, m, rest, ctas, turn) * inv;
+            if (follows) {
+                c = rest > 0.0 ? 1.0 / rest : 0.0;  // (nothing left of q: nothing more is subtracted)
+                c_error = fine ? 0.0 : kRestError;  // (relative)
+                if (!fine && !(rest > 1e-20 && rest < 1e20)) {
+                    certain = false;
+                    break;
+                }
+            }
             m_error = slack + a_error + (1.0 + a) * (fine ? 0.0 : kProductError);
             if (!fine && !(m > 8.0 * m_error)) {  // what is left is no more than the errors
                 certain = false;
@@ -592,17 +659,23 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
     }
 }
 
-template <int DT, bool kShift>
+template <int DT, bool kShift, bool kWithout>
 cudaError_t launch_as(const TreeVerifyParams &P, unsigned ctas, cudaStream_t stream)
 {
     if (ctas > 8) {
         static PerContext allowed;
-        if (!allowed.get([] { return (int)allow_cluster(tree_verify_kernel<DT, kShift>, 16, kThreads); })) {
+        if (!allowed.get([] { return (int)allow_cluster(tree_verify_kernel<DT, kShift, kWithout>, 16, kThreads); })) {
             cudaGetLastError();
             return cudaErrorNotSupported;
         }
     }
-    return launch_pdl(tree_verify_kernel<DT, kShift>, (unsigned)P.B * ctas, kThreads, stream, P, 0, ctas);
+    return launch_pdl(tree_verify_kernel<DT, kShift, kWithout>, (unsigned)P.B * ctas, kThreads, stream, P, 0, ctas);
+}
+
+template <int DT, bool kShift>
+cudaError_t launch_either(const TreeVerifyParams &P, unsigned ctas, cudaStream_t stream)
+{
+    return P.replacement ? launch_as<DT, kShift, false>(P, ctas, stream) : launch_as<DT, kShift, true>(P, ctas, stream);
 }
 
 }  // namespace
@@ -626,8 +699,8 @@ cudaError_t tree_verify_launch(TreeVerifyParams &P, int dtype, cudaStream_t stre
         P.slice = per > (1 << 30) / kBlock ? 1 << 30 : per * kBlock;
         P.chunk = kBlock;
         while ((long long)P.chunk * kMaxChunks < P.slice) P.chunk *= 2;
-        if (dtype == DSSD_BF16) e = shift ? launch_as<DSSD_BF16, true>(P, ctas, stream) : launch_as<DSSD_BF16, false>(P, ctas, stream);
-        else e = shift ? launch_as<DSSD_F32, true>(P, ctas, stream) : launch_as<DSSD_F32, false>(P, ctas, stream);
+        if (dtype == DSSD_BF16) e = shift ? launch_either<DSSD_BF16, true>(P, ctas, stream) : launch_either<DSSD_BF16, false>(P, ctas, stream);
+        else e = shift ? launch_either<DSSD_F32, true>(P, ctas, stream) : launch_either<DSSD_F32, false>(P, ctas, stream);
         if (ctas <= 8) break;
     }
     return e;

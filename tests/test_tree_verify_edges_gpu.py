@@ -54,3 +54,90 @@ def test_a_refused_sibling_after_the_draft_is_exhausted(B, last):
     got = call(B, d, 1.0, False)
     same(got, R.verify(d, 1.0, False))
     assert (got["rs_flags"] == 0).all() and (got["token"] >= 3).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_draft_of_subnormal_numbers(B, dtype):
+    """After the one sibling of ordinary size the rest of q is subnormal in float32, and counts all the same."""
+    V, nb = 300, 200
+    rng = np.random.default_rng(6)
+    x = torch.from_numpy(rng.normal(0, 1, V)).to(dtype)
+    q = np.zeros(V, np.float32)
+    q[1:41] = rng.integers(1, 90000, 40).astype(np.float32) * np.float32(2.0 ** -149)
+    q[0] = 1.0
+    tok = np.stack([np.zeros(nb, np.int64), rng.integers(1, 41, nb), rng.integers(1, 41, nb)], axis=1)
+    d = siblings(x, torch.from_numpy(q), tok, np.concatenate([np.full((nb, 1), 0.999), uniforms(rng, nb, 2)], axis=1), uniforms(rng, nb))
+    same(call(B, d, 0.9, False), R.verify(d, 0.9, False))
+
+
+@pytest.mark.parametrize("gap", [9.0, 14.0, 17.0, 19.0, 30.0])
+@pytest.mark.parametrize("V,dtype", [(5, torch.float32), (3001, torch.bfloat16)])
+def test_siblings_of_a_draft_that_is_nearly_certain(B, gap, V, dtype):
+    """Nearly all of q is one token's.  Once that is refused, the others are drawn from what is left: tails of 1e-4 to 1e-13, next to a q that
+    rounds to 1."""
+    nb = 600
+    rng = np.random.default_rng(int(gap) * 10 + V)
+    top = V // 2
+    x = torch.from_numpy(rng.normal(0, 1.0, V))
+    x[top] += np.log(V)
+    x = x.to(dtype)
+    z = rng.normal(0, 1.5, V)
+    z[top] = z.max() + gap
+    q = np.exp(z - z.max())
+    q = torch.from_numpy((q / q.sum()).astype(np.float32))
+    w = q.double().expand(nb, V).clone()
+    w[:, top] = 0
+    others = torch.multinomial(w, min(V - 1, 3), replacement=False, generator=torch.Generator().manual_seed(V)).numpy()
+    tok = np.concatenate([np.full((nb, 1), top), others], axis=1)
+    u = uniforms(rng, *tok.shape)
+    u[: nb // 2, 0] = 0.999  # (as a rule refused)
+    d = siblings(x, q, tok, u, uniforms(rng, nb))
+    ref = R.verify(d, 0.9, False)
+    same(call(B, d, 0.9, False), ref)
+    assert len(np.unique(ref["path"][:, 1])) > 3
+
+
+@pytest.mark.parametrize("gap", [14.0, 17.0, 19.0])
+def test_the_first_token_follows_the_target_after_a_certain_draft(B, gap):
+    nb = 1 << 17
+    p = np.array([0.6, 0.2, 0.1, 0.06, 0.04])
+    z = np.array([0.0, -gap, -gap - 0.4, -gap - 0.2, -gap - 1.0])
+    q = torch.softmax(torch.from_numpy(z), 0).float()
+    gen = torch.Generator(device="cuda").manual_seed(int(gap))
+    tok = torch.multinomial(q.double().cuda().expand(nb, 5), 2, replacement=False, generator=gen)
+    d = {"target_logits": torch.log(torch.from_numpy(p)).float().cuda().expand(nb, 3, 5).contiguous(), "draft_q": q.cuda().expand(nb, 3, 5).contiguous(),
+         "draft_tokens": tok.int(), "parents": torch.zeros(nb, 2, dtype=torch.int32, device="cuda"), "uniforms": torch.rand(nb, 2, generator=gen, device="cuda"),
+         "uniforms_rs": torch.rand(nb, generator=gen, device="cuda")}
+    r = call(B, d, 1.0, False)
+    first = np.where(r["accept_len"] == 1, np.take_along_axis(tok.cpu().numpy(), np.maximum(r["path"][:, 1:2] - 1, 0), 1)[:, 0], r["token"])
+    freq = np.bincount(first, minlength=5) / nb
+    # five standard deviations of a frequency of nb draws, as in the test of drafts that are not certain
+    assert (np.abs(freq - p) < 5 * np.sqrt(p * (1 - p) / nb)).all(), (freq, p)
+
+
+def test_the_same_sibling_twice(B):
+    """A token that was refused has left q: once more among the siblings it changes nothing."""
+    rng = np.random.default_rng(12)
+    V, nb = 900, 300
+    x = torch.from_numpy(rng.normal(0, 1.5, V)).float()
+    q = torch.softmax(x + torch.from_numpy(rng.normal(0, 1.0, V)).float(), 0)
+    a = torch.multinomial(q, nb, replacement=True, generator=torch.Generator().manual_seed(3)).numpy()
+    b = torch.multinomial(q, nb, replacement=True, generator=torch.Generator().manual_seed(4)).numpy()
+    d = siblings(x, q, np.stack([a, a, b, a], axis=1), uniforms(rng, nb, 4), uniforms(rng, nb))
+    same(call(B, d, 1.0, False), R.verify(d, 1.0, False))
+
+
+def test_many_siblings_without_replacement(B):
+    """More refused siblings than a warp has lanes, all over the row and several to a block."""
+    rng = np.random.default_rng(14)
+    for V, dtype in ((2500, torch.bfloat16), (130, torch.float32)):
+        nb, k = 12, 60
+        x = torch.from_numpy(rng.normal(0, 1.0, (nb, V))).to(dtype)
+        x[:, ::2] -= 12  # (refused as a rule)
+        q = np.exp(rng.normal(0, 1.0, (nb, V)) - 6.0 * (np.arange(V) % 2))
+        q = torch.from_numpy((q / q.sum(axis=1, keepdims=True)).astype(np.float32))
+        tok = torch.multinomial(q.double(), k, replacement=False, generator=torch.Generator().manual_seed(V)).numpy()
+        d = siblings(x, q, tok, 0.5 + 0.5 * uniforms(rng, nb, k), uniforms(rng, nb))
+        ref = R.verify(d, 1.0, False)
+        same(call(B, d, 1.0, False), ref)
+        assert (ref["path"][:, 1] > 33).any() or (ref["accept_len"] == 0).any()
