@@ -45,7 +45,7 @@ struct VerifySmem {
 };
 
 // Bounds of the errors of a float32 pass, relative to the whole distribution, of a sum of p over any entries.  In numerator and row's sum alike, per term: ex2,
-// 2^-22; the rounding of x = l c1 - ref, ln(2) 2^-24 |x|, where sum p |x| is at most the logarithm of the number of entries; the rounding of c1, half of that at the
+// 2^-22; the rounding of x = l c1 - r, ln(2) 2^-24 |x|, where sum p |x| is at most the logarithm of the number of entries; the rounding of c1, half of that at the
 // most between entries; six levels of float32 additions of 2^-24.
 __host__ inline double sum_error(int V) { return 2.0 * (2.4e-7 + 4.2e-8 * (1.5 * log2((double)V + 1.0)) + 6.0 * 6.0e-8); }
 constexpr double kProductError = 2.5e-7;  // of a q in the residual, for each unit of a
@@ -67,8 +67,11 @@ __device__ __forceinline__ double residual(double p, uint32_t q, double a, doubl
 
 // 2^x = 2^(k / 16) 2^r, |r| <= 1/32; the polynomial is the exponential series to the fourth power (relative error below 5e-11).
 // 0 below 2^-1000, infinity above 2^1000.
-__device__ __forceinline__ double exp2_64(double x, const double *table)
+// x = (l - top) c for a logit l given by its bits, top and c by shrunk() and its inverse: the difference comes first, since a product beyond 2^53 would leave
+// nothing of x.  Minus infinity is 0 whatever top is.
+__device__ __forceinline__ double weight(uint32_t l, double top, double c, const double *table)
 {
+    const double x = (shrunk(l) - top) * c;
     const uint32_t hi = (uint32_t)__double2hiint(x);
     const double big = 6755399441055744.0;  // 1.5 * 2^52: adding it rounds to a whole number, held in the low bits
     const double t = __fma_rn(x, 16.0, big);
@@ -79,7 +82,7 @@ __device__ __forceinline__ double exp2_64(double x, const double *table)
     p = __fma_rn(p, r, 6.9314718055994531e-1);
     p = __fma_rn(p, r, 1.0);
     const double y = p * table[k & 15];
-    const bool far = (hi & 0x7fffffffu) > 0x408f4000u;  // |x| > 1000
+    const bool far = (hi & 0x7fffffffu) > 0x408f4000u || l == 0xff800000u;  // |x| > 1000
     const int yh = far ? ((int)hi < 0 ? 0 : 0x7ff00000) : __double2hiint(y) + ((k >> 4) << 20);
     return as_double(yh, far ? 0 : __double2loint(y));
 }
@@ -220,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
     unsigned eflags = S.bad ? DSSD_EDGE_FLAG_BAD_PARENT : 0u, rflags = 0;
 
     int node = 0, length = 0;
-    double a = 0.0, m = 1.0, c = 1.0, ref = 0.0, sum = 1.0, inv = 1.0;
+    double a = 0.0, m = 1.0, c = 1.0, top = 0.0, sum = 1.0, inv = 1.0;
     double a_error = 0.0, m_error = 0.0, c_error = 0.0;
     int refused = 0, mine = -1;  // siblings so far; the one of this lane's number
     bool alive = true, fine = false;
@@ -253,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
         part = 0.0;
     };
     if (me == 0 && t == 0) P.path[b * P.N] = 0;
-    bool relative = false, plain = false;  // take the row relative to its maximum (in ref); draw from p after all
+    bool relative = false, plain = false;  // take the row relative to its maximum (in top); draw from p after all
     while (true) {
         row = static_cast<const char *>(P.logits) + (b * P.N + node) * P.row_stride * (long long)E::Q::kBytes;
         qrow = P.draft_q + (b * P.N + node) * (long long)P.V;
@@ -262,14 +265,14 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
         bool kept = j == 0;  // the pass leaves the chunks' sums
         bool certain = true;
         Asked next = ask(j);
-        if (!relative) ref = 0.0;
+        if (!relative) top = 0.0;
         if (j > 0 && t == 0 && v1 > v0) {
             // What comes next is asked of memory now: this CTA's part of q, which a rejection reads, and of the first child's row.
             prefetch_l2(qrow + v0, (v1 - v0) * 4);
             prefetch_l2(static_cast<const char *>(P.logits) + ((b * P.N + j) * P.row_stride + v0) * (long long)E::Q::kBytes, (v1 - v0) * E::Q::kBytes);
         }
         {
-            // the sum of 2^(l c1 - ref); NaN where the row holds one, or +inf
+            // the sum of 2^((l - top) c1); NaN where the row holds one, or +inf
             double part = 0.0, total = 0.0;
             Walk w(slice, warp);
             if (!fine) {
@@ -312,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 const uint32_t x = E::bits(q, i);
-                                part += exp2_64(__fma_rn(shrunk(x), c1_grown, -ref), S.table);
+                                part += weight(x, top, c1_grown, S.table);
                                 if (is_nan(x)) part = __longlong_as_double(0x7ff8000000000000ll);
                             }
                         }
@@ -339,11 +342,11 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
                 __syncthreads();
                 if (lane == 0) S.warp[0][warp] = (double)mx;
                 __syncthreads();
-                double top = S.warp[0][0];
-                for (int w = 1; w < kWarps; ++w) top = fmax(top, S.warp[0][w]);
+                double most = S.warp[0][0];
+                for (int w = 1; w < kWarps; ++w) most = fmax(most, S.warp[0][w]);
                 __syncthreads();
-                if (top > -1e300 && top < 1e300) {
-                    ref = top * P.c1;
+                if (most > -1e300 && most < 1e300) {
+                    top = shrunk(__float_as_uint((float)most));
                     relative = true;
                     continue;
                 }
@@ -361,7 +364,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
             if (!next.ok) eflags |= DSSD_EDGE_FLAG_BAD_TOKEN;
             if (next.ok && alive) {
                 const double qx = (double)next.q, u = (double)next.u;
-                const double px = exp2_64(__fma_rn(shrunk(next.l), C, -ref), S.table) * inv;
+                const double px = weight(next.l, top, C, S.table) * inv;
                 const double left = fmax(px - a * qx, 0.0), want = u * (c * m) * qx;
                 taken = u < 1.0 && (qx <= 0.0 ? left > 0.0 : want < left);
                 // (a NaN q rejects, whatever the errors)
@@ -477,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
                             const uint4 q = R.at(u);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                const double p = exp2_64(__fma_rn(shrunk(E::bits(l, i)), c1_grown, -ref), S.table);
+                                const double p = weight(E::bits(l, i), top, c1_grown, S.table);
                                 const uint32_t qb = i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w;
                                 const double d = residual(p, qb, aG, sG);
                                 part += d > 0.0 ? d : 0.0;
@@ -592,7 +595,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
                     for (int i = 0; i < 16; ++i) q16[i] = a > 0.0 && v + i < e ? ld_row_u32(qrow + v + i) : 0u;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const double p = exp2_64(__fma_rn(shrunk(l16[i]), C, -ref), S.table);
+                        const double p = weight(l16[i], top, C, S.table);
                         const double d = a > 0.0 ? residual(p, q16[i], aG, sG) : p;
                         w[i] = d > 0.0 ? d : 0.0;
                     }

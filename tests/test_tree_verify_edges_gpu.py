@@ -141,3 +141,24 @@ def test_many_siblings_without_replacement(B):
         ref = R.verify(d, 1.0, False)
         same(call(B, d, 1.0, False), ref)
         assert (ref["path"][:, 1] > 33).any() or (ref["accept_len"] == 0).any()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T", [1.0, 0.37, 1e30, 1e-9, 1e-18])
+def test_rows_far_from_zero(B, dtype, T):
+    """Rows that hold nothing above their type's lowest value, in part or altogether, and rows of 1e30: what counts is the distance from
+    the largest entry."""
+    rng = np.random.default_rng(23)
+    d = R.verify_inputs(rng, 9, 4, 600, dtype, window=2, ragged=False)
+    low, x = torch.finfo(dtype).min, d["target_logits"]
+    x[0] = low
+    x[1] = low
+    x[1, :, ::3] = float("-inf")
+    x[2] = low
+    x[2, :, 7] = low / 2
+    x[3] = 1e30
+    x[4, :, ::2] = 1e30
+    x[5, :, 1::2] = -1e30
+    x[6] = -1e30
+    x[7, :, 300:] = torch.finfo(dtype).max
+    same(call(B, d, T, True), R.verify(d, T, True))
