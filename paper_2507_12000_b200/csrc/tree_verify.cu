@@ -300,7 +300,9 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
                         }
                     float x, y;
                     unpack2(add2(acc[0], acc[1]), x, y);
-                    part += (double)(x + y) * as_double((1023 + (int)fminf(r, 1000.f)) << 20, 0);
+                    // Beyond 2^1000 the sum is out of range, and has to be seen to be: there the rounding of l c1 may leave nothing of a lane's terms.
+                    const float lane_sum = r > 1000.f ? x + y + __int_as_float(0x7f800000) : x + y;
+                    part += (double)lane_sum * as_double((1023 + (int)fminf(r, 1000.f)) << 20, 0);
                     close(kept, ends, k, part, total);
                 }
             } else {

@@ -162,3 +162,18 @@ def test_rows_far_from_zero(B, dtype, T):
     x[6] = -1e30
     x[7, :, 300:] = torch.finfo(dtype).max
     same(call(B, d, T, True), R.verify(d, T, True))
+
+
+@pytest.mark.parametrize("T", [1e-4, 1e-6, 1e-9, 1e-12, 1e-15])
+def test_temperatures_near_zero(B, T):
+    """One entry above zeros: at these temperatures it has all of the mass, wherever the rounding of its scaled value falls."""
+    rng = np.random.default_rng(2)
+    nb, V = 256, 900
+    x = torch.zeros(nb, V)
+    at = rng.integers(0, V, nb)
+    x[torch.arange(nb), torch.from_numpy(at)] = torch.from_numpy(rng.uniform(1.0, 60.0, nb)).float()
+    q = torch.full((nb, V), 1.0 / V)
+    d = siblings(x, q, rng.integers(0, V, (nb, 2)), uniforms(rng, nb, 2), uniforms(rng, nb))
+    got = call(B, d, T, True)
+    same(got, R.verify(d, T, True))
+    assert ((got["token"] == at) | (got["accept_len"] == 1)).all()
