@@ -48,6 +48,8 @@ struct VerifySmem {
 // 2^-22; the rounding of x = l c1 - r, ln(2) 2^-24 |x|, where sum p |x| is at most the logarithm of the number of entries; the rounding of c1, half of that at the
 // most between entries; six levels of float32 additions of 2^-24.
 __host__ inline double sum_error(int V) { return 2.0 * (2.4e-7 + 4.2e-8 * (1.5 * log2((double)V + 1.0)) + 6.0 * 6.0e-8); }
+// Of one p far down, relative, more for each power of two: the rounding of c1, ln(2) 2^-24 |log2 p|.
+constexpr double kBitError = 4.2e-8;
 constexpr double kProductError = 2.5e-7;  // of a q in the residual, for each unit of a
 constexpr double kRestError = 4e-7;       // of what is left of q, relative: six levels of float32 additions
 
@@ -370,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_verify_kernel(const __grid_c
                 const double left = fmax(px - a * qx, 0.0), want = u * (c * m) * qx;
                 taken = u < 1.0 && (qx <= 0.0 ? left > 0.0 : want < left);
                 // (a NaN q rejects, whatever the errors)
-                if (!fine && u < 1.0 && qx > 0.0 && !(fabs(px - a * qx - want) > px * slack + qx * (a_error + u * more_error()))) {
+                if (!fine && u < 1.0 && qx > 0.0 && !(fabs(px - a * qx - want) > px * (slack + kBitError * (double)(1 - exponent(px))) + qx * (a_error + u * more_error()))) {
                     certain = false;
                     break;
                 }

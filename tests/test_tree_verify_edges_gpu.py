@@ -177,3 +177,26 @@ def test_temperatures_near_zero(B, T):
     got = call(B, d, T, True)
     same(got, R.verify(d, T, True))
     assert ((got["token"] == at) | (got["accept_len"] == 1)).all()
+
+
+@pytest.mark.parametrize("bits", [60, 90, 115])
+def test_decisions_on_tokens_far_down(B, bits):
+    """A token of 2^-60 to 2^-115 of the mass, with uniforms within float32's errors of its test's edge.  (T = 1.44: the rounding of
+    log2(e)/T weighs most just above 1.)"""
+    nb, V = 512, 6
+    rng = np.random.default_rng(bits)
+    T = 1.4426950408889634 / (1.0 + rng.uniform(0, 1, nb) * 2.0 ** -6)
+    bad = []
+    for b in range(0, nb, 8):  # one temperature to a call
+        t = float(T[b])
+        x = np.zeros((8, V), np.float32)
+        x[:, 3] = -(bits + rng.uniform(0, 1, 8)) * np.log(2.0) * t
+        p = np.exp(x[:, 3].astype(np.float64) / t) / np.exp(x.astype(np.float64) / t).sum(axis=1)
+        q = np.full((8, V), 0.2, np.float32)
+        q[:, 3] = (p * rng.uniform(1.2, 1.9, 8)).astype(np.float32)
+        u = (p / q[:, 3].astype(np.float64) * (1 + np.array([-5, -3, -2, -1, 1, 2, 3, 5]) * 1e-6)).astype(np.float32)
+        d = siblings(torch.from_numpy(x), torch.from_numpy(q), np.full((8, 1), 3), u[:, None], uniforms(rng, 8))
+        got, ref = call(B, d, t, True), R.verify(d, t, True)
+        if (got["accept_len"] != ref["accept_len"]).any():
+            bad.append((b, got["accept_len"], ref["accept_len"]))
+    assert not bad, (len(bad), bad[:4])
