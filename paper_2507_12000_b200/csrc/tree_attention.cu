@@ -431,7 +431,6 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
         const long long range_start = left;  // (a segment that begins here is the piece's first)
         const int node_in = row / P.G;
         const int head_in = row - node_in * P.G;
-        const float inf = __int_as_float(0x7f800000);
         while (left > 0 && ok) {
             const int h = at.item / P.row_items, rt = at.item - h * P.row_items;
             const int n = (int)(left < at.tiles - at.tile ? left : at.tiles - at.tile);
@@ -658,8 +657,8 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
                     }
                 }
                 if (whole && there && P.lse) P.lse[(at.b * P.N + node) * (P.Hkv * P.G) + head] = top * P.scale + logf(sum);
-                // a row without a node is marked by the piece that has tile 0
-                if (!whole && in_tile) P.part_ml[r] = make_float2(there ? top * P.c : inf, sum);
+                // a row without a node is marked by the piece that has tile 0: no sum of weights is negative
+                if (!whole && in_tile) P.part_ml[r] = make_float2(top * P.c, there ? sum : -1.f);
                 tc_before();
                 bar_arrive(&S.o_free[g]);
                 if (two) bar_arrive(&S.o_free[1]);
@@ -705,9 +704,9 @@ __global__ void __launch_bounds__(kThreads) tree_join_kernel(const __grid_consta
     float top = DSSD_NEG_INF;
     bool none = false;
     for (int k = lane; k < count; k += 32) {
-        const float t = P.part_ml[slot_row(k)].x;
-        none |= t == __int_as_float(0x7f800000);
-        top = fmaxf(top, t);
+        const float2 ml = P.part_ml[slot_row(k)];
+        none |= ml.y < 0.f;
+        top = fmaxf(top, ml.x);
     }
     if (__any_sync(0xffffffffu, none)) return;  // there is no node
     top = warp_max(top);
