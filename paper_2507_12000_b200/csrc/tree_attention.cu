@@ -710,13 +710,14 @@ __global__ void __launch_bounds__(kThreads) tree_join_kernel(const __grid_consta
     }
     if (__any_sync(0xffffffffu, none)) return;  // there is no node
     top = warp_max(top);
+    const float ref = top == DSSD_NEG_INF ? 0.f : top;  // (no score above -inf: an empty sum)
     float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
     const bool mine = lane * 4 < DP;
 #pragma unroll 4
     for (int k = 0; k < count; ++k) {
         const long long r = slot_row(k);
         const float2 ml = P.part_ml[r];
-        const float w = ex2(ml.x - top);
+        const float w = ex2(ml.x - ref);
         sum += w * ml.y;
         if (mine) {
             const float4 v = *reinterpret_cast<const float4 *>(P.part + r * DP + lane * 4);

@@ -29,3 +29,14 @@ def test_a_score_of_infinity_reaches_the_output(B, N, Hq, Hkv, length):  # noqa:
         assert torch.isfinite(got["o"][0, :, :per].float()).all()
         assert torch.equal(got["o"][1], ref["o"][1]) and torch.equal(got["lse"][1], ref["lse"][1])
     assert torch.isfinite(good["o"].float()).all()
+
+
+@pytest.mark.parametrize("length", [100, 4000])
+def test_no_score_above_minus_infinity(B, length):  # noqa: F811
+    """Where every visible key's score is -inf the sum is empty: lse is -inf, and o has no value (NaN)."""
+    d = make(33, 1, 2, 4, 1, 64, 16, [length], torch.bfloat16, chain=True)
+    d["q"] = d["q"].abs() + 0.5
+    d["k_cache"][:] = float("-inf")
+    d["k_new"][:] = float("-inf")
+    got = call(B, d, want_lse=True)
+    assert (got["lse"] == float("-inf")).all() and torch.isnan(got["o"]).all()
