@@ -52,6 +52,21 @@ dssd_status dssd_test_device_resample_wait_runs_out(const float *p_row, const fl
                                                     void *cuda_stream);
 
 /*
+ * dssd_tree_attention in which the keys of sequence `withhold_seq`'s own nodes are never copied into the kernel's shared memory, and every
+ * wait inside gives up after `wait_cycles` clock cycles (about a second's worth otherwise).  The CTAs that wait for these keys give up, let what is in
+ * flight end, free their tensor memory and return; the sequences that they had a part of report DSSD_CACHE_FLAG_TIMEOUT.  Arguments otherwise as
+ * dssd_tree_attention.
+ */
+dssd_status dssd_test_tree_attention_wait_runs_out(const void *q, const int64_t *q_strides, const void *k_new, const void *v_new,
+                                                   const int64_t *new_strides, const void *k_cache, const void *v_cache,
+                                                   const int64_t *cache_strides, dssd_dtype dtype, const int32_t *block_table,
+                                                   int64_t table_stride, int max_pages, int num_pages, int page_size,
+                                                   const int32_t *ctx_len, const int32_t *parents, int B, int N, int Hq, int Hkv,
+                                                   int D, float scale, void *o, const int64_t *o_strides, float *lse, uint32_t *flags,
+                                                   void *workspace, size_t workspace_bytes, int withhold_seq, long long wait_cycles,
+                                                   void *cuda_stream);
+
+/*
  * Which kernels a call of these sizes takes on a device that has clusters of sixteen CTAs: threads per CTA and CTAs per
  * sequence of the kernel that does it in one launch, 0 and 0 where several do it.  They need no GPU.
  *   edge: form 0 dssd_edge_verify, 1 dssd_edge_verify_bonus, 2 dssd_dsd_verify, 3 dssd_edge_partial of a slice of V entries

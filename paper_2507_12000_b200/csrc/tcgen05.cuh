@@ -30,23 +30,35 @@ __device__ __forceinline__ bool bar_try(uint64_t *b, unsigned parity)
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
     return ok;
 }
-// Waits until the phase of that parity is complete.  Every wait ends: after so many looks or cycles (about a second), or once
+// Waits until the phase of that parity is complete.  Every wait ends: after so many looks or cycles, or once
 // another has given up, it says false.
 constexpr unsigned kPolls = 1u << 24;
-constexpr long long kCycles = 2000000000ll;
-__device__ __forceinline__ bool bar_wait(uint64_t *b, unsigned parity, volatile int *failed)
+constexpr long long kCycles = 2000000000ll;  // about a second
+struct Waits {
+    volatile int *failed;  // of the CTA: one has given up
+    long long cycles;
+};
+__device__ __forceinline__ bool bar_wait(uint64_t *b, unsigned parity, const Waits &w)
 {
     if (bar_try(b, parity)) return true;
     const long long begin = clock64();
-    for (unsigned i = 0; i < kPolls && clock64() - begin < kCycles; ++i) {
+    for (unsigned i = 0; i < kPolls && clock64() - begin < w.cycles; ++i) {
         if (bar_try(b, parity)) return true;
-        if (*failed) return false;
+        if (*w.failed) return false;
     }
-    *failed = 1;
+    *w.failed = 1;
     return false;
 }
 // by all lanes of a warp: the same answer in each
-__device__ __forceinline__ bool warp_wait(uint64_t *b, unsigned parity, volatile int *failed) { return __all_sync(0xffffffffu, bar_wait(b, parity, failed)); }
+__device__ __forceinline__ bool warp_wait(uint64_t *b, unsigned parity, const Waits &w) { return __all_sync(0xffffffffu, bar_wait(b, parity, w)); }
+// The same for what is on its way when a role ends, with the same limit, whether another wait has given up or not.
+__device__ __forceinline__ void bar_drain(uint64_t *b, unsigned parity, const Waits &w)
+{
+    const long long begin = clock64();
+    for (unsigned i = 0; i < kPolls && !bar_try(b, parity) && clock64() - begin < w.cycles; ++i)
+        ;
+    __syncwarp();
+}
 
 // what ordinary stores wrote to shared memory is seen by the tensor core and by tiled copies
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -114,6 +126,7 @@ __device__ __forceinline__ void tmem_free(uint32_t at, uint32_t columns)  // the
 {
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
 }
+__device__ __forceinline__ void tmem_ld_wait_all() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // The registers of a load may be used after this: they pass through it, so that nothing that uses them is moved before it.

@@ -3,6 +3,7 @@
 #include <math.h>
 
 #include "dssd.h"
+#include "dssd_test_hooks.h"
 #include "tree_ops.h"
 
 namespace dssd {
@@ -33,6 +34,57 @@ dssd_status check_pages(const int32_t *table, int64_t table_stride, int max_page
     if (max_pages < 0 || num_pages < 0 || page_size < 1 || table_stride < max_pages || (max_pages > 0 && !table)) return DSSD_ERR_INVALID_ARG;
     if ((long long)max_pages * page_size > 0x7fffffff - 65536) return DSSD_ERR_UNSUPPORTED;  // a position is an int
     return DSSD_OK;
+}
+
+dssd_status attend(const void *q, const int64_t *q_strides, const void *k_new, const void *v_new,
+                   const int64_t *new_strides, const void *k_cache, const void *v_cache,
+                   const int64_t *cache_strides, dssd_dtype dtype, const int32_t *block_table,
+                   int64_t table_stride, int max_pages, int num_pages, int page_size,
+                   const int32_t *ctx_len, const int32_t *parents, int B, int N, int Hq, int Hkv, int D,
+                   float scale, void *o, const int64_t *o_strides, float *lse, uint32_t *flags,
+                   void *workspace, size_t workspace_bytes, void *cuda_stream, int withhold, long long wait_cycles)
+{
+    dssd::set_last_cuda_error(0);
+    if (B < 1 || N < 1 || Hq < 1 || Hkv < 1 || D < 1 || Hq % Hkv) return DSSD_ERR_INVALID_ARG;
+    if (N > DSSD_TREE_MAX_NODES || Hq / Hkv > 128 || D > 128 || D % 8) return DSSD_ERR_UNSUPPORTED;
+    if (dtype != DSSD_BF16 && dtype != DSSD_F16) return DSSD_ERR_UNSUPPORTED;
+    if ((long long)B * N * Hq > 0x7fffffff) return DSSD_ERR_UNSUPPORTED;
+    if (!q || !q_strides || !k_new || !v_new || !new_strides || !cache_strides || !ctx_len || !o || !o_strides) return DSSD_ERR_INVALID_ARG;
+    dssd_status st = check_pages(block_table, table_stride, max_pages, num_pages, page_size);
+    if (st != DSSD_OK) return st;
+    if (num_pages > 0 && (!k_cache || !v_cache)) return DSSD_ERR_INVALID_ARG;
+    if (!(scale > 0.f) || !isfinite(scale)) return DSSD_ERR_INVALID_ARG;
+    for (const void *p : {q, k_new, v_new, k_cache, v_cache, static_cast<const void *>(o)})
+        if (!aligned(p, 16)) return DSSD_ERR_INVALID_ARG;
+    for (int i = 0; i < 3; ++i) {
+        if (q_strides[i] < 0 || new_strides[i] < 0 || cache_strides[i] < 0 || o_strides[i] < 0) return DSSD_ERR_INVALID_ARG;
+        if ((q_strides[i] | new_strides[i] | cache_strides[i] | o_strides[i]) % 8) return DSSD_ERR_UNSUPPORTED;
+    }
+    // (a tiled copy takes no stride of nothing)
+    if ((B > 1 && (!q_strides[0] || !new_strides[0])) || (N > 1 && (!q_strides[1] || !new_strides[1])) || (Hq > 1 && !q_strides[2]) ||
+        (Hkv > 1 && (!new_strides[2] || (num_pages > 0 && !cache_strides[2]))) || (num_pages > 1 && !cache_strides[0]) ||
+        (num_pages > 0 && page_size > 1 && !cache_strides[1]))
+        return DSSD_ERR_UNSUPPORTED;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < dssd_tree_attention_workspace_bytes(B, N, Hq, Hkv, D)) return DSSD_ERR_WORKSPACE;
+
+    dssd::TreeAttentionParams P{};
+    P.q = q, P.k_new = k_new, P.v_new = v_new, P.k_cache = k_cache, P.v_cache = v_cache;
+    P.q_b = q_strides[0], P.q_n = q_strides[1], P.q_h = q_strides[2];
+    P.new_b = new_strides[0], P.new_n = new_strides[1], P.new_h = new_strides[2];
+    P.cache_p = cache_strides[0], P.cache_t = cache_strides[1], P.cache_h = cache_strides[2];
+    P.o_b = o_strides[0], P.o_n = o_strides[1], P.o_h = o_strides[2];
+    P.block_table = block_table;
+    P.table_stride = table_stride;
+    P.max_pages = max_pages, P.num_pages = num_pages, P.page_size = page_size;
+    P.ctx_len = ctx_len;
+    P.parents = parents;
+    P.B = B, P.N = N, P.Hq = Hq, P.Hkv = Hkv, P.D = D;
+    P.scale = scale;
+    P.o = o;
+    P.lse = lse;
+    P.flags = flags;
+    P.withhold = withhold, P.wait_cycles = wait_cycles;
+    return done(dssd::tree_attention_launch(P, (int)dtype, workspace, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 }  // namespace
@@ -109,46 +161,21 @@ dssd_status dssd_tree_attention(const void *q, const int64_t *q_strides, const v
                                 float scale, void *o, const int64_t *o_strides, float *lse, uint32_t *flags,
                                 void *workspace, size_t workspace_bytes, void *cuda_stream)
 {
-    dssd::set_last_cuda_error(0);
-    if (B < 1 || N < 1 || Hq < 1 || Hkv < 1 || D < 1 || Hq % Hkv) return DSSD_ERR_INVALID_ARG;
-    if (N > DSSD_TREE_MAX_NODES || Hq / Hkv > 128 || D > 128 || D % 8) return DSSD_ERR_UNSUPPORTED;
-    if (dtype != DSSD_BF16 && dtype != DSSD_F16) return DSSD_ERR_UNSUPPORTED;
-    if ((long long)B * N * Hq > 0x7fffffff) return DSSD_ERR_UNSUPPORTED;
-    if (!q || !q_strides || !k_new || !v_new || !new_strides || !cache_strides || !ctx_len || !o || !o_strides) return DSSD_ERR_INVALID_ARG;
-    dssd_status st = check_pages(block_table, table_stride, max_pages, num_pages, page_size);
-    if (st != DSSD_OK) return st;
-    if (num_pages > 0 && (!k_cache || !v_cache)) return DSSD_ERR_INVALID_ARG;
-    if (!(scale > 0.f) || !isfinite(scale)) return DSSD_ERR_INVALID_ARG;
-    for (const void *p : {q, k_new, v_new, k_cache, v_cache, static_cast<const void *>(o)})
-        if (!aligned(p, 16)) return DSSD_ERR_INVALID_ARG;
-    for (int i = 0; i < 3; ++i) {
-        if (q_strides[i] < 0 || new_strides[i] < 0 || cache_strides[i] < 0 || o_strides[i] < 0) return DSSD_ERR_INVALID_ARG;
-        if ((q_strides[i] | new_strides[i] | cache_strides[i] | o_strides[i]) % 8) return DSSD_ERR_UNSUPPORTED;
-    }
-    // (a tiled copy takes no stride of nothing)
-    if ((B > 1 && (!q_strides[0] || !new_strides[0])) || (N > 1 && (!q_strides[1] || !new_strides[1])) || (Hq > 1 && !q_strides[2]) ||
-        (Hkv > 1 && (!new_strides[2] || (num_pages > 0 && !cache_strides[2]))) || (num_pages > 1 && !cache_strides[0]) ||
-        (num_pages > 0 && page_size > 1 && !cache_strides[1]))
-        return DSSD_ERR_UNSUPPORTED;
-    if (!workspace || !aligned(workspace, 256) || workspace_bytes < dssd_tree_attention_workspace_bytes(B, N, Hq, Hkv, D)) return DSSD_ERR_WORKSPACE;
+    return attend(q, q_strides, k_new, v_new, new_strides, k_cache, v_cache, cache_strides, dtype, block_table, table_stride, max_pages, num_pages, page_size,
+                  ctx_len, parents, B, N, Hq, Hkv, D, scale, o, o_strides, lse, flags, workspace, workspace_bytes, cuda_stream, -1, 0);
+}
 
-    dssd::TreeAttentionParams P{};
-    P.q = q, P.k_new = k_new, P.v_new = v_new, P.k_cache = k_cache, P.v_cache = v_cache;
-    P.q_b = q_strides[0], P.q_n = q_strides[1], P.q_h = q_strides[2];
-    P.new_b = new_strides[0], P.new_n = new_strides[1], P.new_h = new_strides[2];
-    P.cache_p = cache_strides[0], P.cache_t = cache_strides[1], P.cache_h = cache_strides[2];
-    P.o_b = o_strides[0], P.o_n = o_strides[1], P.o_h = o_strides[2];
-    P.block_table = block_table;
-    P.table_stride = table_stride;
-    P.max_pages = max_pages, P.num_pages = num_pages, P.page_size = page_size;
-    P.ctx_len = ctx_len;
-    P.parents = parents;
-    P.B = B, P.N = N, P.Hq = Hq, P.Hkv = Hkv, P.D = D;
-    P.scale = scale;
-    P.o = o;
-    P.lse = lse;
-    P.flags = flags;
-    return done(dssd::tree_attention_launch(P, (int)dtype, workspace, static_cast<cudaStream_t>(cuda_stream)));
+dssd_status dssd_test_tree_attention_wait_runs_out(const void *q, const int64_t *q_strides, const void *k_new, const void *v_new,
+                                                   const int64_t *new_strides, const void *k_cache, const void *v_cache,
+                                                   const int64_t *cache_strides, dssd_dtype dtype, const int32_t *block_table,
+                                                   int64_t table_stride, int max_pages, int num_pages, int page_size,
+                                                   const int32_t *ctx_len, const int32_t *parents, int B, int N, int Hq, int Hkv, int D,
+                                                   float scale, void *o, const int64_t *o_strides, float *lse, uint32_t *flags,
+                                                   void *workspace, size_t workspace_bytes, int withhold_seq, long long wait_cycles, void *cuda_stream)
+{
+    if (withhold_seq < 0 || withhold_seq >= B || wait_cycles < 1) return DSSD_ERR_INVALID_ARG;
+    return attend(q, q_strides, k_new, v_new, new_strides, k_cache, v_cache, cache_strides, dtype, block_table, table_stride, max_pages, num_pages, page_size,
+                  ctx_len, parents, B, N, Hq, Hkv, D, scale, o, o_strides, lse, flags, workspace, workspace_bytes, cuda_stream, withhold_seq, wait_cycles);
 }
 
 size_t dssd_tree_verify_workspace_bytes(int B, int N, int V)

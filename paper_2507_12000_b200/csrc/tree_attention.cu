@@ -53,6 +53,8 @@ struct Geometry {
     int64_t o_b, o_n, o_h;
     float *lse;
     uint32_t *flags;
+    long long wait_cycles;  // the limit of every wait inside
+    int withhold;           // the sequence whose nodes' keys are never copied (-1: none)
     float *part;      // [2 kMaxCtas][kMT * 128][kDP]
     float2 *part_ml;  // [2 kMaxCtas][kMT * 128] maximum in powers of two, sum
     int4 *joins;      // [kMaxCtas] the item that this piece is the second of: sequence, item, slot of its first piece, its last piece; sequence -1: none
@@ -161,7 +163,7 @@ struct Smem {
     static constexpr int kQ = 0, kKV = kMT * kOperand;     // then K and V of the stages in turn
     static constexpr int kRest = kKV + kStages * 2 * kOperand;
     struct Rest {
-        uint64_t q_full, q_empty, k_full[kStages], v_full[kStages], k_empty[kStages], v_empty[kStages], s_full[2], p_ready[2], o_done[2], o_free[2], half;
+        uint64_t q_full, q_empty, k_full[kStages], v_full[kStages], k_empty[kStages], v_empty[kStages], s_full[2], p_ready[2], o_done[2], o_free[2], half, drained;
         signed char parent[kMT == 1 ? 4 : 8][128];  // of the nodes, for each warp of the softmax that meets tile 0
         float2 other[kMT == 1 ? 128 : 1];     // maximum and sum of the second group's half of the keys
         Place place;
@@ -199,6 +201,7 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
             bar_init(&S.o_free[i], 128);
         }
         bar_init(&S.half, 128);
+        bar_init(&S.drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         S.failed = 0;
     }
@@ -234,7 +237,7 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
     __syncthreads();
     tc_after();
     const uint32_t tmem = S.tmem;
-    volatile int *failed = &S.failed;
+    const Waits failed = {&S.failed, P.wait_cycles};
     Place at = S.place;
     long long left = S.count;
 
@@ -252,7 +255,8 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
             const int n = (int)(left < at.tiles - at.tile ? left : at.tiles - at.tile);
             if (keys) {
                 if (items) ok = warp_wait(&S.q_empty, (items - 1) & 1, failed);
-                if (ok && elect()) {
+                if (!ok) break;
+                if (elect()) {
                     bar_expect(&S.q_full, (uint32_t)(kMT * kChunks * P.nodes_per_tile * P.G * 128));
                     for (int m = 0; m < kMT; ++m)
                         for (int x = 0; x < kChunks; ++x)
@@ -285,9 +289,10 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
                 ok = warp_wait(empty_bar + stage, (round & 1) ^ 1, failed);
                 if (!ok) break;
                 const bool one = elect();
-                if (one) bar_expect(bar, (uint32_t)(kChunks * 128 * (i == 0 ? P.N : boxes << P.box_log)));
+                const bool withheld = keys && i == 0 && at.b == P.withhold;
+                if (one && !withheld) bar_expect(bar, (uint32_t)(kChunks * 128 * (i == 0 ? P.N : boxes << P.box_log)));
                 if (i == 0) {
-                    if (one)
+                    if (one && !withheld)
                         for (int x = 0; x < kChunks; ++x) copy_4d(to + x * M::kChunk, fresh, bar, x * 64, h, 0, (int)at.b);
                 } else {
                     for (int y0 = 0; y0 < boxes; y0 += 32) {
@@ -316,6 +321,12 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
             left -= n;
             advance(P, at);
         }
+        // What this warp asked for arrives before the shared memory goes, whoever gave up (as a rule it is there): the last use of each stage, and of Q.
+        for (int s = 0; s < M::kStages; ++s) {
+            const unsigned uses = round + (s < stage);
+            if (uses) bar_drain(full_bar + s, (uses - 1) & 1, failed);
+        }
+        if (keys && items) bar_drain(&S.q_full, (items - 1) & 1, failed);
     } else if (warp == 1) {
         // ---- products: the warp goes through the tiles together and one thread issues, so that operands stay in uniform registers
         int stage = 0, next = 0;  // of PV, of QK
@@ -418,6 +429,11 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
         }
         // the last arrival that the tensor core owes this CTA's shared memory
         if (ok && items) warp_wait(&S.q_empty, (items - 1) & 1, failed);
+        if (!ok) {  // products in flight are done before their operands and tensor memory go
+            if (one) mma_commit(&S.drained);
+            __syncwarp();
+            bar_drain(&S.drained, 0, failed);
+        }
     } else if (warp >= 4) {
         // ---- softmax: a thread per row
         const int g = (warp - 4) / 4, m = kMT == 2 ? g : 0;  // group, tile of rows
@@ -666,18 +682,16 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
             left -= n;
             advance(P, at);
         }
+        if (!ok) {
+            __syncwarp();
+            tmem_ld_wait_all();
+            tmem_st_wait();
+        }
     }
     __syncwarp();
     tc_before();
     __syncthreads();
     tc_after();
-    if (S.failed) {  // copies in flight are waited for, with a limit, before the shared memory goes
-        if (t == 0)
-            for (int i = 0; i < M::kStages; ++i)
-                for (unsigned k = 0; k < 1u << 16 && !(bar_try(&S.k_full[i], 0) && bar_try(&S.v_full[i], 0)) && !(bar_try(&S.k_full[i], 1) && bar_try(&S.v_full[i], 1)); ++k)
-                    ;
-        __syncthreads();
-    }
     if (warp == 1) tmem_free(tmem, 512);
 }
 
@@ -826,6 +840,8 @@ cudaError_t tree_attention_launch(TreeAttentionParams &P, int dtype, void *works
     g.o_b = P.o_b, g.o_n = P.o_n, g.o_h = P.o_h;
     g.lse = P.lse;
     g.flags = P.flags;
+    g.wait_cycles = P.wait_cycles > 0 ? P.wait_cycles : kCycles;
+    g.withhold = P.withhold;
     const int dp = padded(P.D);
     g.part = static_cast<float *>(workspace);
     g.part_ml = reinterpret_cast<float2 *>(g.part + 2 * (size_t)kMaxCtas * rows * dp);

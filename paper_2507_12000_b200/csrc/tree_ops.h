@@ -84,6 +84,9 @@ struct TreeAttentionParams {
     void *o;
     float *lse;
     uint32_t *flags;
+    // for the library's own test of its waits
+    int withhold;           // sequence whose nodes' keys are never copied, -1: none
+    long long wait_cycles;  // limit of a wait, 0: the usual one
 };
 size_t tree_attention_workspace(int B, int N, int Hq, int Hkv, int D);
 cudaError_t tree_attention_launch(TreeAttentionParams &P, int dtype, void *workspace, cudaStream_t stream);
