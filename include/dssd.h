@@ -653,8 +653,8 @@ dssd_status dssd_adjust_logits(const void *logits, dssd_dtype dtype, int64_t row
 #define DSSD_CACHE_FLAG_BAD_LENGTH 2u /* ctx_len negative or beyond the table's pages: taken as the nearer end; append skips
                                          rows beyond the table */
 #define DSSD_CACHE_FLAG_BAD_NODE 4u   /* a parent that is no node below (attention); a path entry outside [0, N) (append) */
-#define DSSD_CACHE_FLAG_TIMEOUT 8u    /* attention: a wait inside the kernel ran out (none of them is endless), rows of the sequence are \
-                                         undefined; nothing is known to bring this about */
+#define DSSD_CACHE_FLAG_TIMEOUT 8u    /* attention: a wait inside the kernel ran out (none of them is endless); rows of o and lse of the sequence are right, \
+                                         not written or NaN; nothing is known to bring this about */
 
 /* Bytes of scratch that dssd_tree_attention needs (0 if the sizes are invalid).  Depends on the sizes only. */
 size_t dssd_tree_attention_workspace_bytes(int B, int N, int Hq, int Hkv, int D);

@@ -175,6 +175,20 @@ struct Smem {
     static_assert(kBytes <= 232448, "a CTA has 227 KB of shared memory");
 };
 
+// Whichever wait ran out, nothing of this CTA's piece is sure to be done: all of its sequences say so, and what the second kernel would join is no
+// number.  (A call, so that it takes no registers from what comes before it.)
+__device__ __noinline__ void give_up(const Geometry &P, Place p, long long count, int rows)
+{
+    if (threadIdx.x == 0 && P.flags)
+        while (count > 0) {
+            atomicOr(P.flags + p.b, DSSD_CACHE_FLAG_TIMEOUT);
+            count -= p.tiles - p.tile;
+            advance(P, p);
+        }
+    const float nan = __int_as_float(0x7fc00000);
+    for (int i = threadIdx.x; i < 2 * rows; i += kAttend) P.part_ml[2ll * blockIdx.x * rows + i] = make_float2(nan, nan);
+}
+
 template <int DT, int DP, int kMT>
 __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid_constant__ Geometry P)
 {
@@ -609,10 +623,7 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
                 }
                 if (++stage == M::kStages) stage = 0, ++round;
             }
-            if (!ok) {
-                if (P.flags) atomicOr(P.flags + at.b, DSSD_CACHE_FLAG_TIMEOUT);
-                break;
-            }
+            if (!ok) break;
             const bool mine = !begin;  // this group had keys of the item (with one tile of it the second had none)
             if (mine && !(ok = warp_wait(&S.o_done[g], (tiles - 1) & 1, failed))) break;
             tc_after();
@@ -692,6 +703,7 @@ __global__ void __launch_bounds__(kAttend, 1) tree_attention_kernel(const __grid
     tc_before();
     __syncthreads();
     tc_after();
+    if (S.failed) give_up(P, S.place, S.count, kMT * 128);
     if (warp == 1) tmem_free(tmem, 512);
 }
 

@@ -54,3 +54,23 @@ def test_keys_that_never_arrive(B, nb, N, Hq, Hkv, D, lens, seq):  # noqa: F811
         assert torch.equal(out["o"][b], good["o"][b]) and torch.equal(out["lse"][b], good["lse"][b]) and int(out["flags"][b]) == 0
     again = call(B, d, out=fresh(d, 3.0), workspace=ws)
     assert all(torch.equal(again[k], good[k]) for k in good)
+
+
+@pytest.mark.parametrize("nb,N,Hq,Hkv,D,lens,seq", CASES)
+def test_a_sequence_without_an_answer_says_so(B, nb, N, Hq, Hkv, D, lens, seq):  # noqa: F811
+    """Whatever else the CTAs that gave up had to do: a sequence that does not report a timeout has its answer."""
+    d = make(62, nb, N, Hq, Hkv, D, 16, lens, torch.bfloat16, chain=True)
+    ws = torch.full((B.dssd_tree_attention_workspace_bytes(nb, N, Hq, Hkv, D),), 1, dtype=torch.uint8, device="cuda")
+    good = call(B, d, out=fresh(d, 0.0), workspace=ws)
+    ws.fill_(1)  # (as float32 a small positive number: results of nobody)
+    out = fresh(d, 7.0)
+    assert withhold(B, d, out, ws, seq) == B.DSSD_OK
+    torch.cuda.synchronize()
+    late = out["flags"] == B.CACHE_FLAG_TIMEOUT
+    assert late[seq] and ((out["flags"] == 0) | late).all()
+    for b in range(nb):
+        row = out["o"][b].float()
+        if not late[b]:
+            assert torch.equal(out["o"][b], good["o"][b]) and torch.equal(out["lse"][b], good["lse"][b]), b
+        else:  # not written, right, or no number: nothing that looks like an answer and is none
+            assert ((row == 7.0) | (out["o"][b] == good["o"][b]) | torch.isnan(row)).all(), b
