@@ -194,6 +194,28 @@ def _sizes(target_logits: torch.Tensor):
     return B, g1 - 1, V, target_logits.device
 
 
+def as_stream(stream, device):
+    """The torch stream of what a call's `stream` may be: None, a torch stream, or a cudaStream_t as an integer or an object that has or converts to
+    one."""
+    if stream is None or isinstance(stream, torch.cuda.Stream):
+        return stream
+    handle = int(getattr(stream, "cuda_stream", stream))
+    return torch.cuda.ExternalStream(0 if handle == 1 else handle, device=device)  # (0 and 1 are the legacy default stream)
+
+
+def _made(stream, device, make):
+    """What make() allocates for a call on `stream`.  It belongs to that stream, and what fills it runs there: the current stream's earlier work and later
+    allocations have nothing to do with it.  The caller may use it on the current stream too."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(as_stream(stream, device)):
+        made = make()
+    for t in made.values() if isinstance(made, dict) else (made,):
+        if t is not None:
+            t.record_stream(torch.cuda.current_stream(device))
+    return made
+
+
 def _workspace(nbytes: int, device) -> torch.Tensor:
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
@@ -544,8 +566,9 @@ def dssd_adjust_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = N
     its token; mask_row [B, N] names each row's mask (negative: none).  Returns {"logits", "flags"}; pass
     out={"logits": logits, ...} to work in place."""
     if out is None:
-        out = {"logits": torch.zeros_like(logits, memory_format=torch.contiguous_format),
-               "flags": torch.empty(logits.shape[0], dtype=torch.int32, device=logits.device)}
+        out = _made(stream, logits.device, lambda: {
+            "logits": torch.zeros_like(logits, memory_format=torch.contiguous_format),
+            "flags": torch.empty(logits.shape[0], dtype=torch.int32, device=logits.device)})
     if workspace is None:
         B, N, V = logits.shape
         workspace = _workspace(dssd_adjust_logits_workspace_bytes(B, N, V, 0 if history is None else history.shape[1],
@@ -571,9 +594,10 @@ def dssd_tree_attention(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tenso
     defaults to 1/sqrt(D)."""
     B, N, Hq, D = q.shape
     if out is None:
-        out = {"o": torch.zeros_like(q, memory_format=torch.contiguous_format),
-               "flags": torch.zeros(B, dtype=torch.int32, device=q.device),
-               "lse": torch.zeros(B, N, Hq, dtype=torch.float32, device=q.device) if want_lse else None}
+        out = _made(stream, q.device, lambda: {
+            "o": torch.zeros_like(q, memory_format=torch.contiguous_format),
+            "flags": torch.zeros(B, dtype=torch.int32, device=q.device),
+            "lse": torch.zeros(B, N, Hq, dtype=torch.float32, device=q.device) if want_lse else None})
     if workspace is None:
         workspace = _workspace(dssd_tree_attention_workspace_bytes(B, N, Hq, k_new.shape[2], D), q.device)
     st = _marshal.tree_attention(q, k_new, v_new, k_cache, v_cache, block_table, ctx_len, parents,
@@ -596,8 +620,8 @@ def dssd_tree_verify(target_logits: torch.Tensor, draft_q: Optional[torch.Tensor
     Returns accept_len [B], path [B, N] (accepted nodes from the root on, then -1), token [B], edge_flags, rs_flags."""
     B, g, V, dev = _sizes(target_logits)
     if out is None:
-        out = {k: torch.empty(B, dtype=torch.int32, device=dev) for k in ("accept_len", "token", "edge_flags", "rs_flags")}
-        out["path"] = torch.empty(B, g + 1, dtype=torch.int32, device=dev)
+        sizes = {"accept_len": (B,), "token": (B,), "edge_flags": (B,), "rs_flags": (B,), "path": (B, g + 1)}
+        out = _made(stream, dev, lambda: {k: torch.empty(n, dtype=torch.int32, device=dev) for k, n in sizes.items()})
     if workspace is None:
         workspace = _workspace(dssd_tree_verify_workspace_bytes(B, g + 1, V), dev)
     st = _marshal.tree_verify(target_logits, draft_q, draft_tokens, parents, uniforms, uniforms_rs, temperature, replacement, out,
@@ -615,7 +639,7 @@ def dssd_cache_append(k_new: torch.Tensor, v_new: torch.Tensor, k_cache: torch.T
     [layers, pages, page_size, Hkv, D] from position ctx_len[b] on (path None: rows 0, 1, ...).  Returns {"new_len", "flags"}."""
     if out is None:
         B, dev = k_new.shape[1], k_new.device
-        out = {"new_len": torch.empty(B, dtype=torch.int32, device=dev), "flags": torch.empty(B, dtype=torch.int32, device=dev)}
+        out = _made(stream, dev, lambda: {k: torch.empty(B, dtype=torch.int32, device=dev) for k in ("new_len", "flags")})
     st = _marshal.cache_append(k_new, v_new, k_cache, v_cache, block_table, ctx_len, accept_len, path, out, stream)
     if st != DSSD_OK:
         raise DssdError(st, "dssd_cache_append")
