@@ -216,7 +216,10 @@ def _made(stream, device, make):
     return made
 
 
-def _workspace(nbytes: int, device) -> torch.Tensor:
+def _workspace(nbytes: int, device, stream=None) -> torch.Tensor:
+    if stream is not None:
+        with torch.cuda.stream(as_stream(stream, device)):
+            return _workspace(nbytes, device)
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 
@@ -572,7 +575,7 @@ def dssd_adjust_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = N
     if workspace is None:
         B, N, V = logits.shape
         workspace = _workspace(dssd_adjust_logits_workspace_bytes(B, N, V, 0 if history is None else history.shape[1],
-                                                                  0 if bias_tokens is None else bias_tokens.shape[1]), logits.device)
+                                                                  0 if bias_tokens is None else bias_tokens.shape[1]), logits.device, stream)
     st = _marshal.adjust_logits(logits, history, prompt_len, history_len, draft_tokens, parents, repetition, presence, frequency,
                                 bias_tokens, bias_values, mask, mask_row, out, workspace, stream)
     if st != DSSD_OK:
@@ -599,7 +602,7 @@ def dssd_tree_attention(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tenso
             "flags": torch.zeros(B, dtype=torch.int32, device=q.device),
             "lse": torch.zeros(B, N, Hq, dtype=torch.float32, device=q.device) if want_lse else None})
     if workspace is None:
-        workspace = _workspace(dssd_tree_attention_workspace_bytes(B, N, Hq, k_new.shape[2], D), q.device)
+        workspace = _workspace(dssd_tree_attention_workspace_bytes(B, N, Hq, k_new.shape[2], D), q.device, stream)
     st = _marshal.tree_attention(q, k_new, v_new, k_cache, v_cache, block_table, ctx_len, parents,
                                  D ** -0.5 if scale is None else scale, out, workspace, stream)
     if st != DSSD_OK:
@@ -623,7 +626,7 @@ def dssd_tree_verify(target_logits: torch.Tensor, draft_q: Optional[torch.Tensor
         sizes = {"accept_len": (B,), "token": (B,), "edge_flags": (B,), "rs_flags": (B,), "path": (B, g + 1)}
         out = _made(stream, dev, lambda: {k: torch.empty(n, dtype=torch.int32, device=dev) for k, n in sizes.items()})
     if workspace is None:
-        workspace = _workspace(dssd_tree_verify_workspace_bytes(B, g + 1, V), dev)
+        workspace = _workspace(dssd_tree_verify_workspace_bytes(B, g + 1, V), dev, stream)
     st = _marshal.tree_verify(target_logits, draft_q, draft_tokens, parents, uniforms, uniforms_rs, temperature, replacement, out,
                               workspace, stream)
     if st != DSSD_OK:

@@ -34,3 +34,24 @@ def test_default_outputs_belong_to_the_stream(B):  # noqa: F811
     got2 = B.dssd_adjust_logits(v["target_logits"], **draft, **adjust, stream=s)
     torch.cuda.synchronize()
     assert all(torch.equal(got[k], ref[k]) for k in ref) and all(torch.equal(got2[k], ref2[k]) for k in ref2)
+
+
+def test_scratch_belongs_to_the_stream(B):  # noqa: F811
+    """The stream is busy when the calls are made: what they took for scratch is not given to the current stream meanwhile."""
+    d = make(42, 3, 5, 4, 2, 64, 16, [100, 40, 333], torch.bfloat16)
+    names = ("q", "k_new", "v_new", "k_cache", "v_cache", "block_table", "ctx_len")
+    v, adjust = inputs(np.random.default_rng(9))
+    draft = {k: v[k] for k in ("draft_tokens", "parents")}
+    ref = B.dssd_tree_attention(*[d[k] for k in names], parents=d["parents"], want_lse=True)
+    ref2 = B.dssd_adjust_logits(v["target_logits"], **draft, **adjust)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(LONG)
+    got = B.dssd_tree_attention(*[d[k] for k in names], parents=d["parents"], want_lse=True, stream=s)
+    got2 = B.dssd_adjust_logits(v["target_logits"], **draft, **adjust, stream=s)
+    sizes = [B.dssd_tree_attention_workspace_bytes(3, 5, 4, 2, 64), B.dssd_adjust_logits_workspace_bytes(4, 9, 2000, 500, 1)]
+    other = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(4)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(got[k], ref[k]) for k in ref) and all(torch.equal(got2[k], ref2[k]) for k in ref2)
+    assert all((x == 255).all() for x in other)
