@@ -246,15 +246,15 @@ def dssd_edge_verify(target_logits: torch.Tensor, draft_tokens: torch.Tensor, dr
     if out is None or workspace is None:
         B, gamma, V, dev = _sizes(target_logits)
         if out is None:
-            out = {
+            out = _made(stream, dev, lambda: {
                 "accept_len": torch.empty(B, dtype=torch.int32, device=dev),
                 "p_row": torch.empty(B, V, dtype=torch.float16 if payload == "f16" else torch.float32, device=dev),
                 "flags": torch.empty(B, dtype=torch.int32, device=dev),
                 "p_tok": torch.empty(B, gamma, dtype=torch.float32, device=dev) if want_p_tok else None,
                 "lse": torch.empty(B, gamma + 1, dtype=torch.float32, device=dev) if want_lse else None,
-            }
+            })
         if workspace is None:
-            workspace = _workspace(dssd_edge_verify_workspace_bytes(B, gamma, V), dev)
+            workspace = _workspace(dssd_edge_verify_workspace_bytes(B, gamma, V), dev, stream)
     st = _marshal.edge_verify(target_logits, draft_tokens, draft_q_tok, uniforms, temperature, out, workspace, stream,
                               payload == "f16")
     if st != DSSD_OK:
@@ -270,10 +270,11 @@ def dssd_device_resample(p_row: torch.Tensor, draft_q: Optional[torch.Tensor], a
     if out is None or workspace is None:
         B, V = p_row.shape
         if out is None:
-            out = {"token": torch.empty(B, dtype=torch.int32, device=p_row.device),
-                   "flags": torch.empty(B, dtype=torch.int32, device=p_row.device)}
+            out = _made(stream, p_row.device, lambda: {
+                "token": torch.empty(B, dtype=torch.int32, device=p_row.device),
+                "flags": torch.empty(B, dtype=torch.int32, device=p_row.device)})
         if workspace is None:
-            workspace = _workspace(dssd_device_resample_workspace_bytes(B, gamma, V), p_row.device)
+            workspace = _workspace(dssd_device_resample_workspace_bytes(B, gamma, V), p_row.device, stream)
     st = _marshal.device_resample(p_row, draft_q, accept_len, uniforms_rs, gamma, out, workspace, stream)
     if st != DSSD_OK:
         raise DssdError(st, "dssd_device_resample")
@@ -313,15 +314,15 @@ def dssd_edge_verify_topk(target_logits: torch.Tensor, draft_tokens: torch.Tenso
         B, gamma, V, dev = _sizes(target_logits)
         if out is None:
             kk = max(0, min(k, TOPK_MAX))
-            out = {
+            out = _made(stream, dev, lambda: {
                 "accept_len": torch.empty(B, dtype=torch.int32, device=dev),
                 "p_idx": torch.empty(B, kk, dtype=torch.int32, device=dev),
                 "p_val": torch.empty(B, kk, dtype=torch.float32, device=dev),
                 "flags": torch.empty(B, dtype=torch.int32, device=dev),
                 "p_tok": torch.empty(B, gamma, dtype=torch.float32, device=dev) if want_p_tok else None,
-            }
+            })
         if workspace is None:
-            workspace = _workspace(dssd_edge_verify_topk_workspace_bytes(B, gamma, V, k), dev)
+            workspace = _workspace(dssd_edge_verify_topk_workspace_bytes(B, gamma, V, k), dev, stream)
     st = _marshal.edge_verify_topk(target_logits, draft_tokens, draft_q_tok, uniforms, temperature, k, out, workspace, stream)
     if st != DSSD_OK:
         raise DssdError(st, "dssd_edge_verify_topk")
@@ -335,8 +336,9 @@ def dssd_device_resample_topk(p_idx: torch.Tensor, p_val: torch.Tensor, q_idx: O
     """Device half on truncated distributions: p_* [B, k], q_* [B, gamma, k] (contiguous)."""
     if out is None:
         B, dev = p_idx.shape[0], p_idx.device
-        out = {"token": torch.empty(B, dtype=torch.int32, device=dev),
-               "flags": torch.empty(B, dtype=torch.int32, device=dev)}
+        out = _made(stream, dev, lambda: {
+            "token": torch.empty(B, dtype=torch.int32, device=dev),
+            "flags": torch.empty(B, dtype=torch.int32, device=dev)})
     st = _marshal.device_resample_topk(p_idx, p_val, q_idx, q_val, accept_len, uniforms_rs, gamma, out, stream)
     if st != DSSD_OK:
         raise DssdError(st, "dssd_device_resample_topk")
@@ -356,9 +358,9 @@ def dssd_dsd_verify(target_logits: torch.Tensor, draft_q: Optional[torch.Tensor]
     if out is None or workspace is None:
         B, gamma, V, dev = _sizes(target_logits)
         if out is None:
-            out = {k: torch.empty(B, dtype=torch.int32, device=dev) for k in ("accept_len", "token", "edge_flags", "rs_flags")}
+            out = _made(stream, dev, lambda: {k: torch.empty(B, dtype=torch.int32, device=dev) for k in ("accept_len", "token", "edge_flags", "rs_flags")})
         if workspace is None:
-            workspace = _workspace(dssd_dsd_verify_workspace_bytes(B, gamma, V), dev)
+            workspace = _workspace(dssd_dsd_verify_workspace_bytes(B, gamma, V), dev, stream)
     st = _marshal.dsd_verify(target_logits, draft_q, draft_tokens, uniforms, uniforms_rs, temperature, out, workspace, stream)
     if st != DSSD_OK:
         raise DssdError(st, "dssd_dsd_verify")
@@ -381,7 +383,7 @@ def dssd_edge_verify_bonus(target_logits: torch.Tensor, draft_tokens: torch.Tens
     if out is None or workspace is None:
         B, gamma, V, dev = _sizes(target_logits)
         if out is None:
-            out = {
+            out = _made(stream, dev, lambda: {
                 "accept_len": torch.empty(B, dtype=torch.int32, device=dev),
                 "p_row": torch.zeros(B, V, dtype=torch.float32, device=dev),
                 "token": torch.empty(B, dtype=torch.int32, device=dev),
@@ -389,9 +391,9 @@ def dssd_edge_verify_bonus(target_logits: torch.Tensor, draft_tokens: torch.Tens
                 "flags": torch.empty(B, dtype=torch.int32, device=dev),
                 "p_tok": torch.empty(B, gamma, dtype=torch.float32, device=dev) if want_p_tok else None,
                 "lse": torch.empty(B, gamma + 1, dtype=torch.float32, device=dev) if want_lse else None,
-            }
+            })
         if workspace is None:
-            workspace = _workspace(dssd_edge_verify_bonus_workspace_bytes(B, gamma, V), dev)
+            workspace = _workspace(dssd_edge_verify_bonus_workspace_bytes(B, gamma, V), dev, stream)
     st = _marshal.edge_verify_bonus(target_logits, draft_tokens, draft_q_tok, uniforms, uniforms_bonus, temperature, out,
                                     workspace, stream)
     if st != DSSD_OK:
@@ -406,7 +408,7 @@ def dssd_device_resample_rejected(p_row: torch.Tensor, draft_q: Optional[torch.T
     dssd_edge_verify_bonus left them) are written where accept_len < gamma and kept elsewhere."""
     if workspace is None:
         B, V = p_row.shape
-        workspace = _workspace(dssd_device_resample_workspace_bytes(B, gamma, V), p_row.device)
+        workspace = _workspace(dssd_device_resample_workspace_bytes(B, gamma, V), p_row.device, stream)
     st = _marshal.device_resample_rejected(p_row, draft_q, accept_len, uniforms_rs, gamma, out, workspace, stream)
     if st != DSSD_OK:
         raise DssdError(st, "dssd_device_resample_rejected")
@@ -472,11 +474,12 @@ def dssd_edge_partial(logits_shard: torch.Tensor, draft_tokens: torch.Tensor, v_
     if out is None or workspace is None:
         B, gamma, Vs, dev = _sizes(logits_shard)
         if out is None:
-            out = {"part_ref": torch.empty(B, gamma + 1, dtype=torch.float32, device=dev),
-                   "part_sum": torch.empty(B, gamma + 1, dtype=torch.float64, device=dev),
-                   "tok_logit": torch.empty(B, gamma, dtype=torch.float32, device=dev)}
+            out = _made(stream, dev, lambda: {
+                "part_ref": torch.empty(B, gamma + 1, dtype=torch.float32, device=dev),
+                "part_sum": torch.empty(B, gamma + 1, dtype=torch.float64, device=dev),
+                "tok_logit": torch.empty(B, gamma, dtype=torch.float32, device=dev)})
         if workspace is None:
-            workspace = _workspace(dssd_edge_partial_workspace_bytes(B, gamma, Vs), dev)
+            workspace = _workspace(dssd_edge_partial_workspace_bytes(B, gamma, Vs), dev, stream)
     st = _marshal.edge_partial(logits_shard, draft_tokens, v_begin, temperature, out, workspace, stream)
     if st != DSSD_OK:
         raise DssdError(st, "dssd_edge_partial")
@@ -492,11 +495,12 @@ def dssd_edge_combine(part_ref: torch.Tensor, part_sum: torch.Tensor, tok_logit:
     if out is None:
         _, B, g1 = part_ref.shape
         dev = part_ref.device
-        out = {"accept_len": torch.empty(B, dtype=torch.int32, device=dev),
-               "row_scale": torch.empty(B, 2, dtype=torch.float32, device=dev),
-               "p_tok": torch.empty(B, g1 - 1, dtype=torch.float32, device=dev),
-               "lse": torch.empty(B, g1, dtype=torch.float32, device=dev),
-               "flags": torch.empty(B, dtype=torch.int32, device=dev)}
+        out = _made(stream, dev, lambda: {
+            "accept_len": torch.empty(B, dtype=torch.int32, device=dev),
+            "row_scale": torch.empty(B, 2, dtype=torch.float32, device=dev),
+            "p_tok": torch.empty(B, g1 - 1, dtype=torch.float32, device=dev),
+            "lse": torch.empty(B, g1, dtype=torch.float32, device=dev),
+            "flags": torch.empty(B, dtype=torch.int32, device=dev)})
     st = _marshal.edge_combine(part_ref, part_sum, tok_logit, draft_tokens, draft_q_tok, uniforms, temperature, V, out, stream)
     if st != DSSD_OK:
         raise DssdError(st, "dssd_edge_combine")
@@ -508,7 +512,7 @@ def dssd_edge_emit_shard(logits_shard: torch.Tensor, accept_len: torch.Tensor, r
     """This shard's slice of the downlink row: [B, V_shard] float32 (`out` may be a view into whole rows)."""
     if out is None:
         B, _, Vs, dev = _sizes(logits_shard)
-        out = torch.empty(B, Vs, dtype=torch.float32, device=dev)
+        out = _made(stream, dev, lambda: torch.empty(B, Vs, dtype=torch.float32, device=dev))
     st = _marshal.edge_emit_shard(logits_shard, accept_len, row_scale, temperature, out, stream)
     if st != DSSD_OK:
         raise DssdError(st, "dssd_edge_emit_shard")
@@ -524,9 +528,9 @@ def dssd_resample_shard_mass(p_row_shard: torch.Tensor, draft_q_shard: Optional[
         B, Vs = p_row_shard.shape
         dev = p_row_shard.device
         if out is None:
-            out = torch.empty(B, 2, dtype=torch.float64, device=dev)
+            out = _made(stream, dev, lambda: torch.empty(B, 2, dtype=torch.float64, device=dev))
         if workspace is None:
-            workspace = _workspace(dssd_resample_shard_workspace_bytes(B, gamma, Vs), dev)
+            workspace = _workspace(dssd_resample_shard_workspace_bytes(B, gamma, Vs), dev, stream)
     st = _marshal.resample_shard_mass(p_row_shard, draft_q_shard, accept_len, gamma, out, workspace, stream)
     if st != DSSD_OK:
         raise DssdError(st, "dssd_resample_shard_mass")
@@ -541,8 +545,9 @@ def dssd_resample_shard_draw(masses: torch.Tensor, g: int, v_begin: int, p_row_s
     in the whole vocabulary on the owning shard and -1 on the others; flags are the sequence's."""
     if out is None:
         B, dev = p_row_shard.shape[0], p_row_shard.device
-        out = {"token": torch.empty(B, dtype=torch.int32, device=dev),
-               "flags": torch.empty(B, dtype=torch.int32, device=dev)}
+        out = _made(stream, dev, lambda: {
+            "token": torch.empty(B, dtype=torch.int32, device=dev),
+            "flags": torch.empty(B, dtype=torch.int32, device=dev)})
     st = _marshal.resample_shard_draw(masses, g, v_begin, p_row_shard, draft_q_shard, accept_len, uniforms_rs, gamma, workspace,
                                       out, stream)
     if st != DSSD_OK:
