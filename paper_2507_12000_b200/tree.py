@@ -20,7 +20,8 @@ def verify_round_tree(target_logits: torch.Tensor, draft_q: Optional[torch.Tenso
                       temperature: float, *, replacement: bool = True, adjust: Optional[Dict[str, torch.Tensor]] = None,
                       cache: Optional[Dict[str, torch.Tensor]] = None, stream=None) -> Dict[str, torch.Tensor]:
     """One round.  target_logits [B, N, V] (adjusted in place if `adjust` is given), draft_q, draft_tokens, parents,
-    uniforms, uniforms_rs, replacement as for `dssd_tree_verify`.
+    uniforms, uniforms_rs, replacement as for `dssd_tree_verify`.  stream: as the calls take it (None, a torch stream, a handle); everything
+    runs there.
 
     adjust: the arguments of `dssd_adjust_logits` by name (history, prompt_len, history_len, repetition, presence, frequency,
             bias_tokens, bias_values, mask, mask_row), those that are wanted.
@@ -30,9 +31,12 @@ def verify_round_tree(target_logits: torch.Tensor, draft_q: Optional[torch.Tenso
     `new_len` and `cache_flags`, with adjustments `adjust_flags`."""
     from . import binding as B
 
+    dev = target_logits.device
+    stream = B.as_stream(stream, dev)  # (what is no stream is refused before anything is written)
     result: Dict[str, torch.Tensor] = {}
     if adjust is not None:
-        out = {"logits": target_logits, "flags": torch.empty(target_logits.shape[0], dtype=torch.int32, device=target_logits.device)}
+        out = B._made(stream, dev, lambda: {"flags": torch.empty(target_logits.shape[0], dtype=torch.int32, device=dev)})
+        out["logits"] = target_logits
         B.dssd_adjust_logits(target_logits, draft_tokens=draft_tokens, parents=parents, out=out, stream=stream, **adjust)
         result["adjust_flags"] = out["flags"]
     result.update(B.dssd_tree_verify(target_logits, draft_q, draft_tokens, parents, uniforms, uniforms_rs, temperature,
@@ -49,8 +53,9 @@ def emitted_tokens(path: torch.Tensor, draft_tokens: Optional[torch.Tensor], acc
                    stream=None) -> torch.Tensor:
     """[B, N]: the tokens of the accepted nodes, then the drawn token, then -1."""
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return emitted_tokens(path, draft_tokens, accept_len, token)
+        from . import binding as B
+
+        return B._made(stream, path.device, lambda: emitted_tokens(path, draft_tokens, accept_len, token))
     n = path.shape[1]
     at = torch.arange(n, device=path.device)
     last = token[:, None].expand(-1, n)

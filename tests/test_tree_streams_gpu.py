@@ -55,3 +55,44 @@ def test_scratch_belongs_to_the_stream(B):  # noqa: F811
     torch.cuda.synchronize()
     assert all(torch.equal(got[k], ref[k]) for k in ref) and all(torch.equal(got2[k], ref2[k]) for k in ref2)
     assert all((x == 255).all() for x in other)
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_a_round_on_another_stream(B, handle):  # noqa: F811
+    """A whole round on a busy stream, given as a torch stream or as its handle, while the current one allocates and writes."""
+    from paper_2507_12000_b200.tree import verify_round_tree
+
+    v, adjust = inputs(np.random.default_rng(10))
+    gen = torch.Generator(device="cuda").manual_seed(10)
+    new = [torch.randn(3, 4, 9, 2, 16, generator=gen, device="cuda").half() for _ in range(2)]
+
+    def round_(logits, stream):
+        cache = [torch.zeros(3, 9, 16, 2, 16, device="cuda").half() for _ in range(2)]
+        c = {"k_new": new[0], "v_new": new[1], "k_cache": cache[0], "v_cache": cache[1],
+             "block_table": torch.arange(8, dtype=torch.int32, device="cuda").reshape(4, 2), "ctx_len": torch.tensor([0, 5, 16, 20], dtype=torch.int32, device="cuda")}
+        torch.cuda.synchronize()
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                torch.cuda._sleep(LONG)
+        r = verify_round_tree(logits, v["draft_q"], v["draft_tokens"], v["parents"], v["uniforms"], v["uniforms_rs"], 0.8, adjust=adjust, cache=c,
+                              stream=stream.cuda_stream if handle and stream is not None else stream)
+        other = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in (16, 144, 512, 1 << 12, 1 << 14, 1 << 16) for _ in range(8)]
+        torch.cuda.synchronize()
+        assert all((x == 255).all() for x in other)
+        return dict(r, logits=logits, k=cache[0], v=cache[1])
+
+    one = round_(v["target_logits"].clone(), None)
+    two = round_(v["target_logits"].clone(), torch.cuda.Stream())
+    assert all(torch.equal(one[k], two[k]) for k in one)
+
+
+def test_what_is_no_stream_is_refused_before_anything_is_written(B):  # noqa: F811
+    from paper_2507_12000_b200.tree import verify_round_tree
+
+    v, adjust = inputs(np.random.default_rng(11))
+    before = v["target_logits"].clone()
+    with pytest.raises((TypeError, ValueError)):
+        verify_round_tree(v["target_logits"], v["draft_q"], v["draft_tokens"], v["parents"], v["uniforms"], v["uniforms_rs"], 0.8, adjust=adjust,
+                          stream="side")
+    torch.cuda.synchronize()
+    assert torch.equal(v["target_logits"], before)
