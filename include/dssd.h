@@ -743,8 +743,8 @@ dssd_status dssd_tree_verify(const void *target_logits, dssd_dtype dtype, int64_
  * k_cache, v_cache   [layers, num_pages, page_size, Hkv, D]; cache_strides (host): elements between layers, pages, positions and heads
  * block_table, ctx_len   as for dssd_tree_attention
  * path          [B, N] int32 or NULL
- * new_len       [B] int32 out, optional: ctx_len + accept_len + 1 (+ N at most).  Not ctx_len itself (DSSD_ERR_INVALID_ARG)
- * flags         [B] uint32 out, optional
+ * new_len       [B] int32 out, optional: ctx_len + accept_len + 1 (+ N at most)
+ * flags         [B] uint32 out, optional.  Neither shares a place with ctx_len, accept_len, path, block_table or the other (DSSD_ERR_INVALID_ARG)
  * Two rows must not go to the same place; accept_len + 1 rows beyond N are left out (BAD_NODE).
  */
 dssd_status dssd_cache_append(const void *k_new, const void *v_new, const int64_t *new_strides, void *k_cache,

@@ -21,6 +21,13 @@ dssd_status done(cudaError_t e)
 
 bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
+// whether two arrays of 4-byte values share a place
+bool overlap(const void *a, long long a_count, const void *b, long long b_count)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && a_count > 0 && b_count > 0 && x < y + 4 * (uintptr_t)b_count && y < x + 4 * (uintptr_t)a_count;
+}
+
 dssd_status check_tree(int B, int N, int V)
 {
     if (B < 1 || N < 1 || V < 1) return DSSD_ERR_INVALID_ARG;
@@ -240,6 +247,12 @@ dssd_status dssd_cache_append(const void *k_new, const void *v_new, const int64_
     for (int i = 0; i < 4; ++i)
         if (new_strides[i] < 0 || cache_strides[i] < 0) return DSSD_ERR_INVALID_ARG;
     if ((long long)Hkv * D > 1 << 24 || (double)layers * B * N > 1e9) return DSSD_ERR_UNSUPPORTED;
+    // (the CTA that reports for a sequence does not wait for those that read its lengths, path and pages)
+    for (const void *r : {static_cast<const void *>(new_len), static_cast<const void *>(flags)})
+        if (overlap(r, B, ctx_len, B) || overlap(r, B, accept_len, B) || overlap(r, B, path, (long long)B * N) ||
+            overlap(r, B, block_table, (B - 1) * table_stride + max_pages))
+            return DSSD_ERR_INVALID_ARG;
+    if (overlap(new_len, B, flags, B)) return DSSD_ERR_INVALID_ARG;
 
     dssd::AppendParams P{};
     P.k_new = k_new, P.v_new = v_new, P.k_cache = k_cache, P.v_cache = v_cache;
