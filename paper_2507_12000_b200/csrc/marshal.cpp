@@ -578,11 +578,12 @@ Strides strides(const at::Tensor &t, const char *what)
     for (int64_t i = 0; i < n - 1; ++i) r.s[i] = t.size(i) > 1 ? t.stride(i) : 0;
     return r;
 }
-// two tensors of one type, shape and spacing on the call's device
+// two tensors of one type, shape and spacing (but along dimensions of one entry) on the call's device
 void alike(const OnDevice &on, const at::Tensor &k, const at::Tensor &v, const char *what)
 {
     require(k.is_cuda() && k.device() == on.device && v.is_cuda() && v.device() == on.device && k.sizes() == v.sizes() &&
-                k.scalar_type() == v.scalar_type() && k.strides() == v.strides(), what);
+                k.scalar_type() == v.scalar_type(), what);
+    for (int64_t i = 0; i < k.dim(); ++i) require(k.size(i) <= 1 || k.stride(i) == v.stride(i), what);
 }
 
 // q, k_new, v_new, k_cache, v_cache, block_table, ctx_len, parents, scale, out, workspace, stream

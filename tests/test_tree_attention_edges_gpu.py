@@ -40,3 +40,25 @@ def test_no_score_above_minus_infinity(B, length):  # noqa: F811
     d["k_new"][:] = float("-inf")
     got = call(B, d, want_lse=True)
     assert (got["lse"] == float("-inf")).all() and torch.isnan(got["o"]).all()
+
+
+def test_spacing_along_dimensions_of_one_entry(B):  # noqa: F811
+    """Keys and values of one head, cut out of tensors of different shapes: the spacing along the one head does not matter."""
+    d = make(35, 2, 3, 4, 1, 64, 16, [100, 33], torch.bfloat16)
+    ref = call(B, d)["o"]
+    both = torch.cat([d["k_new"], d["v_new"]], dim=2)
+    e = dict(d, k_new=both[:, :, :1], v_new=both.transpose(1, 2).contiguous().transpose(1, 2)[:, :, 1:])
+    if e["k_new"].stride()[:2] != e["v_new"].stride()[:2]:
+        e["v_new"] = torch.as_strided(both, (2, 3, 1, 64), (both.stride(0), both.stride(1), 8, 1), 64)
+    assert e["k_new"].stride() != e["v_new"].stride() and torch.equal(e["v_new"], d["v_new"])
+    assert torch.equal(call(B, e)["o"], ref)
+    cache = [torch.zeros(1, 40, 16, 1, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    table = torch.arange(20, dtype=torch.int32, device="cuda").reshape(2, 10)
+    kn, vn = e["k_new"][None], e["v_new"][None]
+    odd = torch.as_strided(cache[1], cache[1].shape, (8,) + cache[1].stride()[1:])
+    B.dssd_cache_append(kn, vn, cache[0], odd, table, d["ctx_len"], torch.full((2,), 2, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    for c, new in zip(cache, (d["k_new"], d["v_new"])):
+        for b, n in enumerate((100, 33)):
+            for i in range(3):
+                assert torch.equal(c[0, int(table[b, (n + i) // 16]), (n + i) % 16], new[b, i])
