@@ -8,7 +8,7 @@
  * The dense kernels hand sums on from one launch to the next; a sum that has not arrived is reported
  * per sequence (DSSD_EDGE_FLAG_TIMEOUT with accept_len = -1, DSSD_RS_FLAG_TIMEOUT |
  * DSSD_RS_FLAG_INVALID with token = -1) and the kernel ends normally.  The first two calls below provoke
- * exactly that by withholding ONE store; nothing else about the launch changes, no address is wrong
+ * exactly that by withholding ONE store, the third by withholding one copy; nothing else about the launch changes, no address is wrong
  * and nothing waits without a bound.
  */
 #ifndef DSSD_TEST_HOOKS_H

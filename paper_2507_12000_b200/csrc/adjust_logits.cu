@@ -89,7 +89,7 @@ struct Request {
         if (!(repetition > 0.f && repetition < __int_as_float(0x7f800000))) repetition = 1.f;
     }
 };
-// The entry that x stands for, in the row of `node`, if it is within [from, to) and not masked: its old value is in `old`
+// The entry that x stands for, in the row of `node`, if that counts it and no mask bans it: `old` is what it held in the given logits
 template <int DT>
 __device__ __forceinline__ void patch(const Request &r, const uint4 &x, typename Vec<DT>::Word old, bool banned, char *out, int node, const short *parent, const int *token)
 {
@@ -318,6 +318,8 @@ __global__ void __launch_bounds__(kList) adjust_list_kernel(const __grid_constan
     T.bias = reinterpret_cast<unsigned short *>(T.count + P.slots);
     T.slots = P.slots;
     if (t == 0) all_flags = 0;
+    // In this order, and with nothing in between: the copy reads and writes the logits without a wait of its own, so it may not be let in before all that came
+    // before this kernel has ended.
     pdl_wait();
     pdl_trigger();
     // what is needed first is asked for at once, the history as far as it may go

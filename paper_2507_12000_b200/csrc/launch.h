@@ -5,7 +5,8 @@
 // before it drains, and they wait (griddepcontrol.wait) before they read or write any global memory.
 // The order stays transitive because every kernel launched this way waits before it lets the next
 // one in (griddepcontrol.launch_dependents) and before it ends: a kernel has completed only after
-// the one before it has.
+// the one before it has.  One kernel works before it waits, the copy of the adjusted logits: it is only ever launched
+// behind the kernel that makes its list, which waits before it lets the copy in, so that all but the list is there.
 #pragma once
 
 #include <atomic>
@@ -22,7 +23,7 @@ cudaError_t launch_pdl(void (*kernel)(Params), unsigned grid, unsigned block, cu
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(block);
-    cfg.dynamicSmemBytes = smem;  // at most 48 KB
+    cfg.dynamicSmemBytes = smem;  // (beyond 48 KB the caller has asked for leave first)
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

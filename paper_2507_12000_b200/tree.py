@@ -6,7 +6,8 @@ the logits of that pass and finishes the round: penalties, biases and masks on e
 test and residual, where a position has several candidates), and the accepted path's keys and values into the
 cache of all layers.  Nothing waits for the GPU, so that a whole round can be captured in a CUDA graph.
 
-Argument marshalling only: every step of the method runs in the library's kernels.
+Every step of the method, from the logits to the verdict and the cache, runs in the library's kernels; what is put together here with torch's own is the list of
+emitted tokens, for the caller's convenience (`emitted_tokens`, about ten small kernels).
 """
 from __future__ import annotations
 
