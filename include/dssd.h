@@ -712,8 +712,8 @@ size_t dssd_tree_verify_workspace_bytes(int B, int N, int V);
  *
  * Only the rows of nodes on the accepted path are read, and draft rows of those with a rejection.
  * The verdict is that of exact arithmetic on the given values, to about 1e-10 of the distribution: what a float32 pass with a bound on its
- * error cannot decide is decided in float64.  T, a float64 here, is from 1e-30 to 1e30 (DSSD_ERR_UNSUPPORTED otherwise).  u == 1 never accepts; q <= 0 accepts iff the left over p > 0; a
- * NaN q or an out-of-range token rejects.
+ * error cannot decide is decided in float64.  T, a float64 here, is from 1e-30 to 1e30 (DSSD_ERR_UNSUPPORTED otherwise).  u == 1 never accepts (and a and m follow the formulas as they
+ * stand); q <= 0 accepts iff the left over p > 0; a NaN q or an out-of-range token rejects.
  *
  * target_logits [B, N, V] float32 or bfloat16, row (b, j) at element (b*N+j)*row_stride
  * draft_q       [B, N, V] float32 contiguous: row j is what node j's children were drawn from

@@ -73,3 +73,12 @@ def test_scratch_belongs_to_the_stream(B, work, handle):
     torch.cuda.synchronize()
     same(got, ref)
     assert all((x == 255).all() for x in other)
+
+
+@pytest.mark.parametrize("handle", [0, 1, 2])
+def test_handles_of_the_default_streams(B, work, handle):
+    """The legacy default stream by both of its handles, and the thread's own."""
+    w, run, ref = work
+    got = run(stream=handle)
+    torch.cuda.synchronize()
+    same(got, ref)
