@@ -96,3 +96,28 @@ def test_what_is_no_stream_is_refused_before_anything_is_written(B):  # noqa: F8
                           stream="side")
     torch.cuda.synchronize()
     assert torch.equal(v["target_logits"], before)
+
+
+def test_calls_on_two_streams_at_once(B):  # noqa: F811
+    """Attention, adjusted logits and the verdict on two streams, call by call in turns, with the buffers that they make themselves."""
+    names = ("q", "k_new", "v_new", "k_cache", "v_cache", "block_table", "ctx_len")
+    work = [(make(50 + i, 4, 7, 16, 2, 128, 16, [900, 40, 0, 5000], torch.bfloat16), *inputs(np.random.default_rng(50 + i))) for i in range(2)]
+
+    def calls(i, stream):
+        d, v, adjust = work[i]
+        draft = {k: v[k] for k in ("draft_tokens", "parents")}
+        yield B.dssd_tree_attention(*[d[k] for k in names], parents=d["parents"], want_lse=True, stream=stream)
+        yield B.dssd_adjust_logits(v["target_logits"], **draft, **adjust, stream=stream)
+        for replacement in (True, False):
+            yield B.dssd_tree_verify(v["target_logits"], v["draft_q"], v["draft_tokens"], v["parents"], v["uniforms"], v["uniforms_rs"], 0.8,
+                                     replacement=replacement, stream=stream)
+
+    ref = [list(calls(i, None)) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        got = list(zip(*[calls(i, streams[i]) for i in range(2)]))
+        torch.cuda.synchronize()
+        for k, both in enumerate(got):
+            for i in range(2):
+                assert all(torch.equal(both[i][x], ref[i][k][x]) for x in ref[i][k])
